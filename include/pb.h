@@ -253,6 +253,73 @@ int pb_lstm_cell(const void *packed, const float *scales, const pb_desc *d, int 
                  int input_size, const float *h_prev, const float *c_prev, const float *bias, float *h_out,
                  float *c_out, int batch, void *workspace, void *stream);
 
+/* A gated block: the two projections of its input packed as one matrix, rows = 2F, row r < F the gate and row F + r the
+ * value of unit r.  With [g ; u] = W x + bias (the product of pb_matmul),
+ *   H[n][r] = act(g[r]) * u[r],
+ * act a pb_gate, in fp32.  PB_GATE_GELU is the tanh form, 0.5 v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))).
+ *   X     [batch][cols] fp32, bias [2F] or NULL: read only
+ *   H     [batch][F], written
+ *   pre   [batch][2F] or NULL: the pre-activations [g ; u], written (what the backward pass needs)
+ *   workspace: pb_workspace_bytes(d, batch) bytes, overwritten
+ * No output may overlap another one or an input.  PB_EINVAL if rows is odd. */
+typedef enum pb_gate { PB_GATE_SIGMOID = 0, PB_GATE_SILU = 1, PB_GATE_GELU = 2, PB_GATE_RELU = 3 } pb_gate;
+int pb_gated_linear(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *X, int batch,
+                    const float *bias, int gate, float *H, float *pre, void *workspace, void *stream);
+
+/* Gradient of pb_matmul with respect to its activations, the packed matrix being frozen:
+ *   dX[n][c] = sum_r dY[n][r] w[r][c],   w = sum_{i < bits_used} scales[i] * bit_i,
+ * with the same bits_used as in the forward call; the conversion to fixed point counts as the identity (frac_bits and act_bits do
+ * not matter).  dY enters as integers of 31 bits of its vector's largest magnitude, the sums of products are exact and
+ * rounded to fp32 (more than 1024 steps of 64 rows, more than eight bitlayers, few vectors: a few such sums are added in fp32, in the same
+ * order every time).  A vector with a value that is not finite gets NaN everywhere.
+ *   dY  [batch][rows] fp32, read only;  dX  [batch][cols] fp32, written
+ *   workspace: pb_grad_workspace_bytes(d, batch) bytes, overwritten (0 for what the call does not take)
+ * Tiled layouts only (PB_EINVAL for PB_LAYOUT_ROWMAJOR_V1). */
+size_t pb_grad_workspace_bytes(const pb_desc *d, int batch);
+int pb_matmul_grad(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *dY, int batch,
+                   float *dX, void *workspace, void *stream);
+
+/* Backward pass of pb_gated_linear, from the pre-activations that it left:
+ *   dpre = [dH u act'(g) ; dH act(g)],   dX = the gradient of pb_matmul for dpre.
+ * (The gradient of the bias is the sum of dpre over the vectors.)
+ *   pre [batch][2F], dH [batch][F]: read only;  dpre [batch][2F], dX [batch][cols]: written
+ *   workspace: pb_grad_workspace_bytes(d, batch) bytes, overwritten
+ * No output may overlap another one or an input.  Tiled layouts only. */
+int pb_gated_linear_grad(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *pre, const float *dH,
+                         int batch, int gate, float *dpre, float *dX, void *workspace, void *stream);
+
+/* Low-rank adapters beside a packed matrix (host struct, plain data): adapter k adds scale[k] B_k A_k to it.
+ *   A [count][rank][cols], B [count][rows][rank] of type `type`, scale [count] fp32 or NULL (1): device pointers, read only */
+typedef enum pb_type { PB_TYPE_F32 = 0, PB_TYPE_BF16 = 1, PB_TYPE_F16 = 2 } pb_type;
+#define PB_MAX_ADAPTERS 4096
+#define PB_MAX_RANK 256
+typedef struct pb_adapters {
+    int32_t count, rank, type, reserved;   /* reserved: 0 */
+    const void *A, *B;
+    const float *scale;
+} pb_adapters;
+
+/* pb_matmul with an adapter per vector, those of many requests in one call:
+ *   Y[n] = (the product of pb_matmul for x_n) + bias + scale[k] B_k (A_k x_n),   k = index[n].
+ * The adapters' products take x as it is (not its fixed-point value) and run in fp32, whatever the adapters' type.
+ *   index  [batch] int32, in any order; a vector whose index is outside [0, count) has no adapter.  NULL: adapter 0 for all
+ *   bias   [rows] or NULL;  Y  [batch][rows] fp32, written
+ *   workspace: pb_adapters_workspace_bytes(d, adapters, batch) bytes, overwritten (0 for a shape that is refused) */
+size_t pb_adapters_workspace_bytes(const pb_desc *d, const pb_adapters *adapters, int batch);
+int pb_matmul_adapters(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *X, int batch,
+                       const pb_adapters *adapters, const int32_t *index, const float *bias, float *Y, void *workspace, void *stream);
+
+/* Backward pass of pb_matmul_adapters, the packed matrix being frozen.  With u = A_k x_n and t = scale[k] B_k^T dy_n:
+ *   dA[k] = sum_n t x_n^T,   dB[k] = scale[k] sum_n dy_n u^T,   dX[n] = (the gradient of pb_matmul for dy_n) + A_k^T t,
+ * the sums over the vectors of adapter k in their order (the same bits every time); zero for an adapter without vectors.
+ *   X [batch][cols], dY [batch][rows] fp32, index as in the forward call: read only
+ *   dA [count][rank][cols], dB [count][rows][rank], dX [batch][cols]: fp32, written; NULL for what is not wanted
+ *   workspace: pb_adapters_workspace_bytes(d, adapters, batch) bytes, overwritten
+ * Tiled layouts only.  No output may overlap another one or an input. */
+int pb_matmul_adapters_grad(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *X, const float *dY,
+                            int batch, const pb_adapters *adapters, const int32_t *index, float *dX, float *dA, float *dB,
+                            void *workspace, void *stream);
+
 /* Text for a pb_status; the HIP error code of the last PB_EHIP on this thread. */
 const char *pb_strerror(int status);
 int pb_last_hip_error(void);

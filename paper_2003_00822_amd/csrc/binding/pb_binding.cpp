@@ -23,17 +23,19 @@
 namespace {
 
 // what pb.py hands over once, when it has loaded the library
-PyObject *g_desc_type = nullptr;    // the ctypes structure pb_desc
+PyObject *g_desc_type = nullptr;    // the ctypes structures pb_desc
+PyObject *g_adapters_type = nullptr;    // and pb_adapters
 PyObject *g_error = nullptr;        // PbError(status, where)
 
 enum Entry {
     kQuantizePack, kQuantizePackDesc, kQuantizePackMode, kUnpack, kMatmul, kMatmulStatic, kMatmulBiasAct, kMatmulAcc,
-    kMatmulAccPairs, kActPrep, kMatmulPrepared, kFixedPoint, kLstmCell, kEntries
+    kMatmulAccPairs, kActPrep, kMatmulPrepared, kFixedPoint, kLstmCell, kGatedLinear, kMatmulGrad,
+    kGatedLinearGrad, kMatmulAdapters, kMatmulAdaptersGrad, kEntries
 };
 const char *const kNames[kEntries] = {
     "pb_quantize_pack", "pb_quantize_pack_desc", "pb_quantize_pack_mode", "pb_unpack", "pb_matmul", "pb_matmul_static",
     "pb_matmul_bias_act", "pb_matmul_acc", "pb_matmul_acc_pairs", "pb_act_prep", "pb_matmul_prepared", "pb_fixed_point",
-    "pb_lstm_cell"};
+    "pb_lstm_cell", "pb_gated_linear", "pb_matmul_grad", "pb_gated_linear_grad", "pb_matmul_adapters", "pb_matmul_adapters_grad"};
 void *g_fn[kEntries];               // null until bound: every call then goes to `slow`
 PyObject *g_slow[kEntries];
 PyObject *g_slow_linear = nullptr;
@@ -56,8 +58,10 @@ struct Ptr {
 using In = Ptr<const float, at::kFloat>;
 using InOrNone = Ptr<const float, at::kFloat, true>;
 using Out = Ptr<float, at::kFloat>;
+using OutOrNone = Ptr<float, at::kFloat, true>;
 using Bytes = Ptr<void, at::kByte>;
 using Ints = Ptr<int32_t, at::kInt>;
+using IntsOrNone = Ptr<const int32_t, at::kInt, true>;
 using Longs = Ptr<int64_t, at::kLong>;
 
 struct Int {
@@ -84,20 +88,23 @@ struct Address {
     }
 };
 
-struct Desc {
-    pb_desc v;
+template <typename S, PyObject **TYPE>
+struct Struct {
+    S v;
     bool load(PyObject *o)
     {
-        if (reinterpret_cast<PyObject *>(Py_TYPE(o)) != g_desc_type) return false;
+        if (reinterpret_cast<PyObject *>(Py_TYPE(o)) != *TYPE) return false;
         Py_buffer b;
         if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) { PyErr_Clear(); return false; }
-        const bool ok = b.len == (Py_ssize_t)sizeof(pb_desc);
-        if (ok) v = *static_cast<const pb_desc *>(b.buf);
+        const bool ok = b.len == (Py_ssize_t)sizeof(S);
+        if (ok) v = *static_cast<const S *>(b.buf);
         PyBuffer_Release(&b);
         return ok;
     }
-    const pb_desc *get() const { return &v; }
+    const S *get() const { return &v; }
 };
+using Desc = Struct<pb_desc, &g_desc_type>;
+using Adapters = Struct<pb_adapters, &g_adapters_type>;
 
 void *current_stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
@@ -225,11 +232,11 @@ PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     return PyObject_Vectorcall(g_slow_linear, args, nargs, nullptr);
 }
 
-// bind(desc_type, error_type, {name: address})
+// bind(desc_type, adapters_type, error_type, {name: address})
 PyObject *bind(PyObject *, PyObject *args)
 {
-    PyObject *desc, *error, *fns;
-    if (!PyArg_ParseTuple(args, "OOO!", &desc, &error, &PyDict_Type, &fns)) return nullptr;
+    PyObject *desc, *adapters, *error, *fns;
+    if (!PyArg_ParseTuple(args, "OOOO!", &desc, &adapters, &error, &PyDict_Type, &fns)) return nullptr;
     void *p[kEntries];
     for (int e = 0; e < kEntries; ++e) {
         PyObject *a = PyDict_GetItemString(fns, kNames[e]);
@@ -238,10 +245,13 @@ PyObject *bind(PyObject *, PyObject *args)
         if (!p[e]) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "%s", kNames[e]);
     }
     Py_INCREF(desc);
+    Py_INCREF(adapters);
     Py_INCREF(error);
     Py_XDECREF(g_desc_type);
+    Py_XDECREF(g_adapters_type);
     Py_XDECREF(g_error);
     g_desc_type = desc;
+    g_adapters_type = adapters;
     g_error = error;
     for (int e = 0; e < kEntries; ++e) g_fn[e] = p[e];
     Py_RETURN_NONE;
@@ -297,6 +307,12 @@ PyMethodDef kMethods[] = {
     fast<&pb_matmul_prepared, kMatmulPrepared, Bytes, In, Desc, Int, Int, Out, Bytes>(),
     fast<&pb_fixed_point, kFixedPoint, Desc, In, Int, Ints, Bytes>(),
     fast<&pb_lstm_cell, kLstmCell, Bytes, In, Desc, Int, In, Int, In, In, InOrNone, Out, Out, Int, Bytes>(),
+    fast<&pb_gated_linear, kGatedLinear, Bytes, In, Desc, Int, In, Int, InOrNone, Int, Out, OutOrNone, Bytes>(),
+    fast<&pb_matmul_grad, kMatmulGrad, Bytes, In, Desc, Int, In, Int, Out, Bytes>(),
+    fast<&pb_gated_linear_grad, kGatedLinearGrad, Bytes, In, Desc, Int, In, In, Int, Int, Out, Out, Bytes>(),
+    fast<&pb_matmul_adapters, kMatmulAdapters, Bytes, In, Desc, Int, In, Int, Adapters, IntsOrNone, InOrNone, Out, Bytes>(),
+    fast<&pb_matmul_adapters_grad, kMatmulAdaptersGrad, Bytes, In, Desc, Int, In, In, Int, Adapters, IntsOrNone, OutOrNone, OutOrNone,
+         OutOrNone, Bytes>(),
     {"linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&linear)), METH_FASTCALL, nullptr},
     {"bind", bind, METH_VARARGS, nullptr},
     {"set_slow", set_slow, METH_O, nullptr},

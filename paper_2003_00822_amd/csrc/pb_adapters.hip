@@ -1,0 +1,539 @@
+// Low-rank adapters beside a packed layer, an adapter k per vector chosen by an index on the device:
+//   Y_n += scale_k B_k (A_k x_n)                                    (pb_matmul_adapters)
+//   u = A_k x_n,  t = scale_k B_k^T dy_n,  dX_n += A_k^T t,  dA_k = sum_n t x_n^T,  dB_k = scale_k sum_n dy_n u^T     (its backward pass)
+// A [count][rank][cols], B [count][rows][rank], both in fp32, bf16 or fp16; everything is multiplied and added in fp32.
+//
+// The vectors are put in the order of their adapters (k_adapter_order), and a tile is up to sixteen vectors of one adapter: an adapter
+// is read once per tile and product, whatever the order of the requests.  The products are V_MFMA_F32_16X16X4_F32: lane 16 kb + i brings
+// row i (column i) of the two operands at position kb of the sum, and gets rows 4 kb .. 4 kb + 3 of column i of the result.  Which
+// summand stands at which position is free as long as both operands agree, so lanes load neighbouring summands with wide loads.
+// Bound: memory and latencies.  The products of 2048 vectors of rank 16 with 4096 columns take 2 us of the chip's fp32 matrix rate.
+#include <hip/hip_runtime.h>
+#include <hip/hip_fp16.h>
+#include <stdint.h>
+
+#include "pb_kernels.h"
+
+namespace pb {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+struct bf16 { uint16_t v; };
+struct f16 { uint16_t v; };
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(bf16 v) { return __uint_as_float((uint32_t)v.v << 16); }
+__device__ __forceinline__ float to_f32(f16 v) { return (float)__builtin_bit_cast(_Float16, v.v); }
+// Four values next to each other (aligned to their size)
+__device__ __forceinline__ v4f load4(const float *p) { return *reinterpret_cast<const v4f *>(p); }
+__device__ __forceinline__ v4f load4(const bf16 *p)
+{
+    const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
+    return v4f{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xFFFF0000u), __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xFFFF0000u)};
+}
+__device__ __forceinline__ v4f load4(const f16 *p)
+{
+    const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
+    return v4f{to_f32(f16{(uint16_t)w[0]}), to_f32(f16{(uint16_t)(w[0] >> 16)}), to_f32(f16{(uint16_t)w[1]}), to_f32(f16{(uint16_t)(w[1] >> 16)})};
+}
+// The values p[at .. at + 4) of `length`, 0 beyond the end.  VEC: `length` and `at` are multiples of four.
+template <bool VEC, typename T>
+__device__ __forceinline__ v4f load4_of(const T *p, int at, int length)
+{
+    if constexpr (VEC) return at < length ? load4(p + at) : v4f{0, 0, 0, 0};
+    else {
+        v4f v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = at + i < length ? to_f32(p[at + i]) : 0.0f;
+        return v;
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void store4_of(float *p, int at, int length, v4f v)
+{
+    if constexpr (VEC) {
+        if (at < length) *reinterpret_cast<v4f *>(p + at) = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (at + i < length) p[at + i] = v[i];
+    }
+}
+__device__ __forceinline__ v4f mfma(float a, float b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+// ---- the order of the vectors ----
+struct Item { int adapter, start, length, pad; };     // places start .. start + length of the order
+
+// What the kernels go by: the order of the vectors, its tiles, and where an adapter's vectors begin in it.  Without an index all vectors have
+// adapter 0 and their own order, and none of the arrays is there.
+struct Order {
+    const int *order;
+    const Item *items;
+    const int *counts;        // [0]: tiles
+    const int *starts;        // [adapter], and the end
+    int batch;
+    __device__ bool tile(int i, Item *t) const
+    {
+        if (!order) {
+            *t = {0, i * 16, min(16, batch - i * 16), 0};
+            return i * 16 < batch;
+        }
+        if (i >= counts[0]) return false;
+        *t = items[i];
+        return true;
+    }
+    __device__ int vector(int place) const { return order ? order[place] : place; }
+    __device__ void segment(int adapter, int *start, int *end) const
+    {
+        *start = order ? starts[adapter] : (adapter ? batch : 0);
+        *end = order ? starts[adapter + 1] : batch;
+    }
+};
+
+// One workgroup.  A wave finds out for 64 vectors which of them have the same adapter (a ballot per bit of its number), then the waves add to the
+// adapters' counts in the order of the vectors: the order within an adapter is theirs, so that sums over its vectors are the same every time.
+constexpr int kOrderThreads = 1024, kChunks = PB_MAX_BATCH / 64, kChunksPerWave = kChunks / (kOrderThreads / 64);
+__global__ __launch_bounds__(kOrderThreads) void k_adapter_order(const int32_t *__restrict__ index, int batch, int count, int *__restrict__ order,
+                                                                 Item *__restrict__ items, int *__restrict__ counts, int *__restrict__ starts)
+{
+    __shared__ int s_count[PB_MAX_ADAPTERS];
+    __shared__ uint32_t s_first[PB_MAX_ADAPTERS];     // places before the adapter's, and from bit 16 on tiles before its
+    __shared__ uint32_t s_wave[kOrderThreads / 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int k = threadIdx.x; k < PB_MAX_ADAPTERS; k += kOrderThreads) s_count[k] = 0;
+    int key[kChunksPerWave], place[kChunksPerWave], same[kChunksPerWave];
+#pragma unroll
+    for (int i = 0; i < kChunksPerWave; ++i) {
+        const int n = (i * (kOrderThreads / 64) + wave) * 64 + lane;
+        int k = n < batch ? index[n] : -1;
+        if (k < 0 || k >= count) k = -1;
+        unsigned long long mask = __builtin_amdgcn_ballot_w64(k >= 0);
+        for (int b = 0; b < 12; ++b) {
+            const unsigned long long set = __builtin_amdgcn_ballot_w64((k >> b & 1) != 0);
+            mask &= (k >> b & 1) ? set : ~set;
+        }
+        key[i] = k;
+        place[i] = __popcll(mask & ((1ull << lane) - 1));
+        same[i] = __popcll(mask);
+    }
+    static_assert(PB_MAX_ADAPTERS == 1 << 12, "twelve bits");
+    const int chunks = (batch + 63) / 64;
+#pragma unroll
+    for (int i = 0; i < kChunksPerWave; ++i)
+        for (int w = 0; w < kOrderThreads / 64 && i * (kOrderThreads / 64) + w < chunks; ++w) {
+            __syncthreads();
+            if (wave == w && key[i] >= 0) {
+                const int before = s_count[key[i]];
+                if (place[i] == 0) s_count[key[i]] = before + same[i];
+                place[i] += before;
+            }
+        }
+    __syncthreads();
+    // places and tiles before each adapter: four adapters per thread
+    uint32_t own[4], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = s_count[threadIdx.x * 4 + i];
+        own[i] = sum;
+        sum += (uint32_t)c + ((uint32_t)((c + 15) / 16) << 16);
+    }
+    uint32_t scan = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t v = (uint32_t)__shfl_up((int)scan, d);
+        if (lane >= d) scan += v;
+    }
+    if (lane == 63) s_wave[wave] = scan;
+    __syncthreads();
+    uint32_t before = scan - sum;
+    for (int w = 0; w < wave; ++w) before += s_wave[w];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s_first[threadIdx.x * 4 + i] = before + own[i];
+    if (threadIdx.x == kOrderThreads - 1) {
+        counts[0] = (int)((before + sum) >> 16);
+        starts[count] = (int)((before + sum) & 0xFFFFu);
+    }
+    __syncthreads();
+    for (int k = threadIdx.x; k < count; k += kOrderThreads) starts[k] = (int)(s_first[k] & 0xFFFFu);
+#pragma unroll
+    for (int i = 0; i < kChunksPerWave; ++i) {
+        const int k = key[i], n = (i * (kOrderThreads / 64) + wave) * 64 + lane;
+        if (k < 0) continue;
+        const int start = (int)(s_first[k] & 0xFFFFu), at = start + place[i];
+        order[at] = n;
+        if (place[i] % 16 == 0) items[(s_first[k] >> 16) + place[i] / 16] = {k, at, min(16, s_count[k] - place[i]), 0};
+    }
+}
+
+// ---- u = A_k x and t = scale_k B_k^T dy ----
+struct DownArgs {
+    Order order;
+    const void *M;            // A or B
+    const float *scale;       // (t only)
+    const float *V;           // [batch][length]
+    float *out;               // [slice][place][16 ranks]: rank tile after rank tile, 16 values each
+    int length, rank, ranks, slices;
+};
+// Parts of the sum of a tile's products go to the waves of `slices` workgroups; a lane's result is four ranks of one vector.
+//   TURNED: the summands are the rows of the matrix (B: [length][rank]), else its columns (A: [rank][length])
+template <typename T, bool TURNED, bool VEC, int RT>
+__global__ __launch_bounds__(256) void k_adapter_down(const DownArgs a)
+{
+    __shared__ v4f s_part[3][RT][64];
+    const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
+    Item it;
+    if (!a.order.tile(blockIdx.x, &it)) return;
+    const T *const M = static_cast<const T *>(a.M) + (size_t)it.adapter * a.rank * a.length;
+    const float *const x = a.V + (size_t)a.order.vector(it.start + min(i, it.length - 1)) * a.length;
+    const int rt0 = blockIdx.z * RT;
+    v4f acc[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) acc[t] = v4f{0, 0, 0, 0};
+    for (int c0 = (blockIdx.y * 4 + wave) * 64; c0 < a.length; c0 += a.slices * 256) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int c = c0 + 16 * q + 4 * kb;
+            const v4f v = load4_of<VEC>(x, c, a.length);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                const int j = (rt0 + t) * 16 + i;
+                v4f w = v4f{0, 0, 0, 0};
+                if (j < a.rank) {
+                    if constexpr (TURNED) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = c + e < a.length ? to_f32(M[(size_t)(c + e) * a.rank + j]) : 0.0f;
+                    } else {
+                        w = load4_of<VEC>(M + (size_t)j * a.length, c, a.length);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[t] = mfma(w[e], v[e], acc[t]);
+            }
+        }
+    }
+    if (wave > 0) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) s_part[wave - 1][t][lane] = acc[t];
+    }
+    __syncthreads();
+    if (wave > 0 || i >= it.length) return;
+    const float s = a.scale ? a.scale[it.adapter] : 1.0f;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        if (rt0 + t >= a.ranks) break;
+        v4f v = acc[t];
+        for (int w = 0; w < 3; ++w) v += s_part[w][t][lane];
+        v *= s;
+        // (ranks beyond the last are zero whatever the vector holds: 0 times infinity must not reach the products that follow)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if ((rt0 + t) * 16 + 4 * kb + e >= a.rank) v[e] = 0.0f;
+        *reinterpret_cast<v4f *>(a.out + (((size_t)blockIdx.y * a.order.batch + it.start + i) * a.ranks + rt0 + t) * 16 + 4 * kb) = v;
+    }
+}
+// Ranks 4 part .. 4 part + 3 of rank tile `rt` at `place`: the slices added up in their order
+__device__ __forceinline__ v4f down_at(const float *parts, int slices, int batch, int ranks, int place, int rt, int part)
+{
+    const float *p = parts + ((size_t)place * ranks + rt) * 16 + 4 * part;
+    v4f v = *reinterpret_cast<const v4f *>(p);
+    for (int s = 1; s < slices; ++s) v += *reinterpret_cast<const v4f *>(p + (size_t)s * batch * ranks * 16);
+    return v;
+}
+__device__ __forceinline__ float down1_at(const float *parts, int slices, int batch, int ranks, int place, int rt, int i)
+{
+    const float *p = parts + ((size_t)place * ranks + rt) * 16 + i;
+    float v = *p;
+    for (int s = 1; s < slices; ++s) v += p[(size_t)s * batch * ranks * 16];
+    return v;
+}
+
+// ---- Y += scale_k B_k u, dX += A_k^T t ----
+struct UpArgs {
+    Order order;
+    const void *M;
+    const float *scale;       // (Y only)
+    const float *parts;       // u or t
+    float *out;               // [batch][length]
+    int length, rank, ranks, slices;
+};
+// A wave does 64 values of the tile's vectors.  TURNED: M is A [rank][length], else B [length][rank]
+template <typename T, bool TURNED, bool VEC, bool RANK4>
+__global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
+{
+    const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
+    const int r0 = (blockIdx.x * 4 + wave) * 64;
+    Item it;
+    if (r0 >= a.length || !a.order.tile(blockIdx.y, &it)) return;
+    const T *const M = static_cast<const T *>(a.M) + (size_t)it.adapter * a.rank * a.length;
+    const int place = it.start + min(i, it.length - 1);
+    const float s = a.scale ? a.scale[it.adapter] : 1.0f;
+    v4f acc[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc[t] = v4f{0, 0, 0, 0};
+    for (int rt = 0; rt < a.ranks; ++rt) {
+        if constexpr (TURNED) {
+            // summand 4 e + kb; tile t has the values r0 + 4 i + t
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = rt * 16 + 4 * e + kb;
+                const float u = down1_at(a.parts, a.slices, a.order.batch, a.ranks, place, rt, 4 * e + kb);
+                const v4f w = j < a.rank ? load4_of<VEC>(M + (size_t)j * a.length, r0 + 4 * i, a.length) : v4f{0, 0, 0, 0};
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[t] = mfma(w[t], u, acc[t]);
+            }
+        } else {
+            // summand 4 kb + e; tile t has the values r0 + 16 t + i
+            const v4f u = down_at(a.parts, a.slices, a.order.batch, a.ranks, place, rt, kb) * s;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int r = r0 + 16 * t + i;
+                const v4f w = r < a.length ? load4_of<RANK4>(M + (size_t)r * a.rank, rt * 16 + 4 * kb, a.rank) : v4f{0, 0, 0, 0};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[t] = mfma(w[e], u[e], acc[t]);
+            }
+        }
+    }
+    if (i >= it.length) return;
+    float *const y = a.out + (size_t)a.order.vector(place) * a.length;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const int r = r0 + (TURNED ? 16 * kb + 4 * t : 16 * t + 4 * kb);
+        v4f v = acc[t];
+        if constexpr (TURNED) v = v4f{acc[0][t], acc[1][t], acc[2][t], acc[3][t]};
+        store4_of<VEC>(y, r, a.length, load4_of<VEC>(y, r, a.length) + v);
+    }
+}
+
+// ---- dA_k = sum t x^T, dB_k = scale_k sum dy u^T ----
+struct OuterArgs {
+    Order order;
+    const float *scale;       // (dB only)
+    const float *parts;       // t or u
+    const float *V;           // x or dy, [batch][length]
+    float *out;               // TURNED: [adapter][length][rank], else [adapter][rank][length]
+    int length, rank, ranks, slices;
+};
+constexpr int kOuterWaves = 8;
+// A workgroup does 64 columns (rows) and RT rank tiles of an adapter; its waves take every eighth four of the adapter's vectors.
+template <bool TURNED, bool VEC, bool RANK4, int RT>
+__global__ __launch_bounds__(kOuterWaves * 64) void k_adapter_outer(const OuterArgs a)
+{
+    __shared__ v4f s_part[kOuterWaves - 1][RT * 4][64];
+    const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
+    const int k = blockIdx.y, rt0 = blockIdx.z * RT, c = blockIdx.x * 64 + 4 * i;
+    int start, end;
+    a.order.segment(k, &start, &end);
+    v4f acc[RT][4];
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[t][q] = v4f{0, 0, 0, 0};
+    for (int p0 = start + 4 * wave; p0 < end; p0 += 4 * kOuterWaves) {
+        const int place = p0 + kb;
+        const bool live = place < end;
+        const v4f v = live ? load4_of<VEC>(a.V + (size_t)a.order.vector(place) * a.length, c, a.length) : v4f{0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            float u = 0.0f;
+            if (live && rt0 + t < a.ranks) u = down1_at(a.parts, a.slices, a.order.batch, a.ranks, place, rt0 + t, i);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[t][q] = mfma(u, v[q], acc[t][q]);
+        }
+    }
+    if (wave > 0) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) s_part[wave - 1][t * 4 + q][lane] = acc[t][q];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    const float s = a.scale ? a.scale[k] : 1.0f;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            for (int w = 0; w < kOuterWaves - 1; ++w) acc[t][q] += s_part[w][t * 4 + q][lane];
+            acc[t][q] *= s;
+        }
+        // the lane has ranks j .. j + 3 of the columns c .. c + 3
+        const int j = (rt0 + t) * 16 + 4 * kb;
+        if constexpr (TURNED) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (c + q < a.length) store4_of<RANK4>(a.out + ((size_t)k * a.length + c + q) * a.rank, j, a.rank, acc[t][q]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (j + e < a.rank)
+                    store4_of<VEC>(a.out + ((size_t)k * a.rank + j + e) * a.length, c, a.length, v4f{acc[t][0][e], acc[t][1][e], acc[t][2][e], acc[t][3][e]});
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+
+AdapterPlan adapter_plan(const Layout &L, const pb_adapters &ad, int batch, bool indexed)
+{
+    AdapterPlan p;
+    const int tiles = (batch + 15) / 16;
+    p.items = indexed ? (ad.count + batch / 16 < batch ? ad.count + batch / 16 : batch) : tiles;
+    p.ranks = (ad.rank + 15) / 16;
+    // parts of the sums: about two workgroups per compute unit, each wave with 64 summands or more
+    const int most = L.rows > L.cols ? L.rows : L.cols;
+    int slices = 512 / (p.items * ((p.ranks + 3) / 4));
+    if (slices > (most + 255) / 256) slices = (most + 255) / 256;
+    p.slices = slices < 1 ? 1 : (slices > 16 ? 16 : slices);
+    auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
+    const size_t down = up((size_t)p.slices * batch * p.ranks * 64);
+    p.items_off = up((size_t)batch * 4);
+    p.counts_off = up(p.items_off + (size_t)p.items * sizeof(Item));
+    p.starts_off = p.counts_off + 256;
+    p.u_off = up(p.starts_off + (size_t)(ad.count + 1) * 4);
+    p.t_off = p.u_off + down;
+    p.bytes = p.t_off + down;
+    return p;
+}
+
+static Order order_of(const AdapterPlan &p, bool indexed, int batch, void *workspace)
+{
+    char *const ws = static_cast<char *>(workspace);
+    Order o = {nullptr, nullptr, nullptr, nullptr, batch};
+    if (indexed) {
+        o.order = reinterpret_cast<const int *>(ws);
+        o.items = reinterpret_cast<const Item *>(ws + p.items_off);
+        o.counts = reinterpret_cast<const int *>(ws + p.counts_off);
+        o.starts = reinterpret_cast<const int *>(ws + p.starts_off);
+    }
+    return o;
+}
+
+int launch_adapter_order(const AdapterPlan &p, const pb_adapters &ad, const int32_t *index, int batch, void *workspace, hipStream_t st)
+{
+    if (!index) return 0;
+    char *const ws = static_cast<char *>(workspace);
+    hipLaunchKernelGGL(k_adapter_order, dim3(1), dim3(kOrderThreads), 0, st, index, batch, ad.count, reinterpret_cast<int *>(ws),
+                       reinterpret_cast<Item *>(ws + p.items_off), reinterpret_cast<int *>(ws + p.counts_off),
+                       reinterpret_cast<int *>(ws + p.starts_off));
+    return (int)hipGetLastError();
+}
+
+// fn(T(), ...) for the type of the adapters
+template <typename F>
+static int by_type(int type, F fn)
+{
+    switch (type) {
+        case PB_TYPE_F32: return fn(float());
+        case PB_TYPE_BF16: return fn(bf16());
+        default: return fn(f16());
+    }
+}
+static int launch(const void *fn, dim3 grid, int threads, void *args, hipStream_t st)
+{
+    void *list[] = {args};
+    const hipError_t e = hipLaunchKernel(fn, grid, dim3((unsigned)threads), list, 0, st);
+    return (int)(e != hipSuccess ? e : hipGetLastError());
+}
+template <typename T, bool TURNED, bool VEC>
+static const void *down_kernel(int rt)
+{
+    if (rt == 1) return reinterpret_cast<const void *>(k_adapter_down<T, TURNED, VEC, 1>);
+    if (rt == 2) return reinterpret_cast<const void *>(k_adapter_down<T, TURNED, VEC, 2>);
+    return reinterpret_cast<const void *>(k_adapter_down<T, TURNED, VEC, 4>);
+}
+static int ranks_at_once(const AdapterPlan &p) { return p.ranks >= 3 ? 4 : p.ranks; }
+
+int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, bool indexed, const float *X, const float *dY, int batch,
+                        void *workspace, hipStream_t st)
+{
+    char *const ws = static_cast<char *>(workspace);
+    const int rt = ranks_at_once(p);
+    const dim3 grid((unsigned)p.items, (unsigned)p.slices, (unsigned)((p.ranks + rt - 1) / rt));
+    return by_type(ad.type, [&](auto type) {
+        typedef decltype(type) T;
+        DownArgs a;
+        a.order = order_of(p, indexed, batch, workspace);
+        a.rank = ad.rank; a.ranks = p.ranks; a.slices = p.slices;
+        int err = 0;
+        if (X) {
+            a.M = ad.A; a.scale = nullptr; a.V = X; a.length = L.cols;
+            a.out = reinterpret_cast<float *>(ws + p.u_off);
+            err = launch(L.cols % 4 ? down_kernel<T, false, false>(rt) : down_kernel<T, false, true>(rt), grid, 256, &a, st);
+        }
+        if (!err && dY) {
+            a.M = ad.B; a.scale = ad.scale; a.V = dY; a.length = L.rows;
+            a.out = reinterpret_cast<float *>(ws + p.t_off);
+            err = launch(L.rows % 4 ? down_kernel<T, true, false>(rt) : down_kernel<T, true, true>(rt), grid, 256, &a, st);
+        }
+        return err;
+    });
+}
+
+template <typename T, bool TURNED>
+static const void *up_kernel(bool vec, bool rank4)
+{
+    if (TURNED || rank4) return vec ? reinterpret_cast<const void *>(k_adapter_up<T, TURNED, true, true>)
+                                    : reinterpret_cast<const void *>(k_adapter_up<T, TURNED, false, true>);
+    return vec ? reinterpret_cast<const void *>(k_adapter_up<T, false, true, false>)
+               : reinterpret_cast<const void *>(k_adapter_up<T, false, false, false>);
+}
+
+int launch_adapter_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, bool indexed, int batch, float *Y, void *workspace,
+                      hipStream_t st)
+{
+    UpArgs a;
+    a.order = order_of(p, indexed, batch, workspace);
+    a.M = ad.B; a.scale = ad.scale; a.parts = reinterpret_cast<const float *>(static_cast<char *>(workspace) + p.u_off); a.out = Y;
+    a.length = L.rows; a.rank = ad.rank; a.ranks = p.ranks; a.slices = p.slices;
+    return by_type(ad.type, [&](auto type) {
+        return launch(up_kernel<decltype(type), false>(L.rows % 4 == 0, ad.rank % 4 == 0),
+                      dim3((unsigned)((L.rows + 255) / 256), (unsigned)p.items), 256, &a, st);
+    });
+}
+
+template <bool TURNED, int RT>
+static const void *outer_kernel(bool vec, bool rank4)
+{
+    if (!TURNED || rank4) return vec ? reinterpret_cast<const void *>(k_adapter_outer<TURNED, true, true, RT>)
+                                     : reinterpret_cast<const void *>(k_adapter_outer<TURNED, false, true, RT>);
+    return vec ? reinterpret_cast<const void *>(k_adapter_outer<true, true, false, RT>)
+               : reinterpret_cast<const void *>(k_adapter_outer<true, false, false, RT>);
+}
+
+int launch_adapter_grads(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, bool indexed, const float *X, const float *dY, int batch,
+                         float *dX, float *dA, float *dB, void *workspace, hipStream_t st)
+{
+    char *const ws = static_cast<char *>(workspace);
+    const float *const u = reinterpret_cast<const float *>(ws + p.u_off), *const t = reinterpret_cast<const float *>(ws + p.t_off);
+    const Order order = order_of(p, indexed, batch, workspace);
+    const bool rank4 = ad.rank % 4 == 0;
+    int err = 0;
+    if (dX) {
+        UpArgs a;
+        a.order = order; a.M = ad.A; a.scale = nullptr; a.parts = t; a.out = dX;
+        a.length = L.cols; a.rank = ad.rank; a.ranks = p.ranks; a.slices = p.slices;
+        err = by_type(ad.type, [&](auto type) {
+            return launch(up_kernel<decltype(type), true>(L.cols % 4 == 0, true), dim3((unsigned)((L.cols + 255) / 256), (unsigned)p.items), 256,
+                          &a, st);
+        });
+    }
+    const unsigned z = p.ranks == 1 ? 1u : (unsigned)((p.ranks + 1) / 2);
+    OuterArgs o;
+    o.order = order; o.rank = ad.rank; o.ranks = p.ranks; o.slices = p.slices;
+    if (!err && dA) {
+        o.scale = nullptr; o.parts = t; o.V = X; o.out = dA; o.length = L.cols;
+        const bool vec = L.cols % 4 == 0;
+        err = launch(p.ranks == 1 ? outer_kernel<false, 1>(vec, rank4) : outer_kernel<false, 2>(vec, rank4),
+                     dim3((unsigned)((L.cols + 63) / 64), (unsigned)ad.count, z), kOuterWaves * 64, &o, st);
+    }
+    if (!err && dB) {
+        o.scale = ad.scale; o.parts = u; o.V = dY; o.out = dB; o.length = L.rows;
+        const bool vec = L.rows % 4 == 0;
+        err = launch(p.ranks == 1 ? outer_kernel<true, 1>(vec, rank4) : outer_kernel<true, 2>(vec, rank4),
+                     dim3((unsigned)((L.rows + 63) / 64), (unsigned)ad.count, z), kOuterWaves * 64, &o, st);
+    }
+    return err;
+}
+
+}  // namespace pb

@@ -357,6 +357,144 @@ int pb_lstm_cell(const void *packed, const float *scales, const pb_desc *d, int 
                                                 static_cast<hipStream_t>(stream)));
 }
 
+int pb_gated_linear(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *X, int batch,
+                    const float *bias, int gate, float *H, float *pre, void *workspace, void *stream)
+{
+    pb::Layout L;
+    int rc = check_desc(d, &L);
+    if (rc != PB_OK) return rc;
+    if (!scales || !H || !workspace || d->rows % 2 != 0 || gate < PB_GATE_SIGMOID || gate > PB_GATE_RELU) return PB_EINVAL;
+    if (batch < 1) return PB_EINVAL;
+    if (batch > PB_MAX_BATCH) return PB_ESIZE;
+    if (!aligned16(H) || !aligned16(pre) || !aligned16(workspace)) return PB_EALIGN;
+    pb::Epilogue ep;
+    ep.bias = bias;
+    const Issuing issuing(workspace);
+    float *const to = pre ? pre : reinterpret_cast<float *>(static_cast<char *>(workspace) + pb::ws_gates_off(L, batch));
+    rc = matmul_common(packed, scales, d, bits_used, X, d->cols, nullptr, 0, batch, to, nullptr, workspace, stream, ep, false, true);
+    if (rc != PB_OK) return rc;
+    return hip_status(pb::launch_gated(to, d->rows / 2, gate, batch, H, static_cast<hipStream_t>(stream)));
+}
+
+size_t pb_grad_workspace_bytes(const pb_desc *d, int batch)
+{
+    pb::Layout L;
+    if (check_desc(d, &L) != PB_OK || batch < 1 || batch > PB_MAX_BATCH || !pb::is_tile16(L.layout)) return 0;
+    return pb::grad_workspace_bytes(L, batch);
+}
+
+// Checks that the gradient calls share; the caller's lock is held
+static int check_grad(const void *packed, const float *scales, const pb_desc *d, int bits_used, int batch, const void *workspace, pb::Layout *L)
+{
+    const int rc = check_desc(d, L);
+    if (rc != PB_OK) return rc;
+    if (!packed || !scales || !workspace) return PB_EINVAL;
+    if (!pb::is_tile16(L->layout)) return PB_EINVAL;
+    if (bits_used < 1 || bits_used > d->bits || batch < 1) return PB_EINVAL;
+    if (batch > PB_MAX_BATCH) return PB_ESIZE;
+    return aligned16(packed) && aligned16(scales) && aligned16(workspace) ? PB_OK : PB_EALIGN;
+}
+
+int pb_matmul_grad(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *dY, int batch,
+                   float *dX, void *workspace, void *stream)
+{
+    pb::Layout L;
+    const int rc = check_grad(packed, scales, d, bits_used, batch, workspace, &L);
+    if (rc != PB_OK) return rc;
+    if (!dY || !dX) return PB_EINVAL;
+    if (!aligned16(dY) || !aligned16(dX)) return PB_EALIGN;
+    const Issuing issuing(workspace);
+    return hip_status(pb::launch_grad(static_cast<const uint32_t *>(packed), scales, L, bits_used, dY, nullptr, batch, dX, workspace,
+                                      static_cast<hipStream_t>(stream)));
+}
+
+int pb_gated_linear_grad(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *pre, const float *dH,
+                         int batch, int gate, float *dpre, float *dX, void *workspace, void *stream)
+{
+    pb::Layout L;
+    const int rc = check_grad(packed, scales, d, bits_used, batch, workspace, &L);
+    if (rc != PB_OK) return rc;
+    if (!pre || !dH || !dpre || !dX || d->rows % 2 != 0 || gate < PB_GATE_SIGMOID || gate > PB_GATE_RELU) return PB_EINVAL;
+    if (!aligned16(pre) || !aligned16(dH) || !aligned16(dpre) || !aligned16(dX)) return PB_EALIGN;
+    const pb::GatedSource gated = {pre, dH, dpre, gate};
+    const Issuing issuing(workspace);
+    return hip_status(pb::launch_grad(static_cast<const uint32_t *>(packed), scales, L, bits_used, nullptr, &gated, batch, dX, workspace,
+                                      static_cast<hipStream_t>(stream)));
+}
+
+static int check_adapters(const pb_adapters *ad)
+{
+    if (!ad || !ad->A || !ad->B || ad->count < 1 || ad->rank < 1) return PB_EINVAL;
+    if (ad->type < PB_TYPE_F32 || ad->type > PB_TYPE_F16) return PB_EINVAL;
+    if (ad->count > PB_MAX_ADAPTERS || ad->rank > PB_MAX_RANK) return PB_ESIZE;
+    return aligned16(ad->A) && aligned16(ad->B) && aligned16(ad->scale) ? PB_OK : PB_EALIGN;
+}
+
+// The adapters' part of the workspace lies behind that of the product (forward or backward, whichever is larger)
+static size_t adapters_off(const pb::Layout &L, int batch)
+{
+    const size_t f = pb::workspace_bytes(L, batch), g = pb::is_tile16(L.layout) ? pb::grad_workspace_bytes(L, batch) : 0;
+    return ((f > g ? f : g) + 255) & ~(size_t)255;
+}
+
+size_t pb_adapters_workspace_bytes(const pb_desc *d, const pb_adapters *ad, int batch)
+{
+    pb::Layout L;
+    if (check_desc(d, &L) != PB_OK || batch < 1 || batch > PB_MAX_BATCH) return 0;
+    if (!ad || ad->count < 1 || ad->count > PB_MAX_ADAPTERS || ad->rank < 1 || ad->rank > PB_MAX_RANK) return 0;
+    const size_t with = pb::adapter_plan(L, *ad, batch, true).bytes, without = pb::adapter_plan(L, *ad, batch, false).bytes;
+    return adapters_off(L, batch) + (with > without ? with : without);
+}
+
+int pb_matmul_adapters(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *X, int batch,
+                       const pb_adapters *adapters, const int32_t *index, const float *bias, float *Y, void *workspace, void *stream)
+{
+    pb::Layout L;
+    int rc = check_desc(d, &L);
+    if (rc == PB_OK) rc = check_adapters(adapters);
+    if (rc != PB_OK) return rc;
+    if (!packed || !scales || !X || !Y || !workspace) return PB_EINVAL;
+    if (bits_used < 1 || bits_used > d->bits || batch < 1) return PB_EINVAL;
+    if (batch > PB_MAX_BATCH) return PB_ESIZE;
+    if (!aligned16(packed) || !aligned16(scales) || !aligned16(X) || !aligned16(Y) || !aligned16(index) || !aligned16(bias) || !aligned16(workspace))
+        return PB_EALIGN;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const Issuing issuing(workspace);
+    const pb::AdapterPlan p = pb::adapter_plan(L, *adapters, batch, index != nullptr);
+    void *const ws = static_cast<char *>(workspace) + adapters_off(L, batch);
+    int err = pb::launch_adapter_order(p, *adapters, index, batch, ws, st);
+    if (!err) err = pb::launch_adapter_down(p, *adapters, L, index != nullptr, X, nullptr, batch, ws, st);
+    if (err) return hip_status(err);
+    pb::Epilogue ep;
+    ep.bias = bias;
+    rc = matmul_common(packed, scales, d, bits_used, X, d->cols, nullptr, 0, batch, Y, nullptr, workspace, stream, ep, false, true);
+    if (rc != PB_OK) return rc;
+    return hip_status(pb::launch_adapter_up(p, *adapters, L, index != nullptr, batch, Y, ws, st));
+}
+
+int pb_matmul_adapters_grad(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *X, const float *dY,
+                            int batch, const pb_adapters *adapters, const int32_t *index, float *dX, float *dA, float *dB,
+                            void *workspace, void *stream)
+{
+    pb::Layout L;
+    int rc = check_grad(packed, scales, d, bits_used, batch, workspace, &L);
+    if (rc == PB_OK) rc = check_adapters(adapters);
+    if (rc != PB_OK) return rc;
+    if (!X || !dY || (!dX && !dA && !dB)) return PB_EINVAL;
+    if (!aligned16(X) || !aligned16(dY) || !aligned16(index) || !aligned16(dX) || !aligned16(dA) || !aligned16(dB)) return PB_EALIGN;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const Issuing issuing(workspace);
+    const pb::AdapterPlan p = pb::adapter_plan(L, *adapters, batch, index != nullptr);
+    void *const ws = static_cast<char *>(workspace) + adapters_off(L, batch);
+    int err = pb::launch_adapter_order(p, *adapters, index, batch, ws, st);
+    // (u is needed for dB, t for dA and dX)
+    if (!err) err = pb::launch_adapter_down(p, *adapters, L, index != nullptr, dB ? X : nullptr, dX || dA ? dY : nullptr, batch, ws, st);
+    if (!err && dX)
+        err = pb::launch_grad(static_cast<const uint32_t *>(packed), scales, L, bits_used, dY, nullptr, batch, dX, workspace, st);
+    if (!err) err = pb::launch_adapter_grads(p, *adapters, L, index != nullptr, X, dY, batch, dX, dA, dB, ws, st);
+    return hip_status(err);
+}
+
 const char *pb_strerror(int status)
 {
     switch (status) {

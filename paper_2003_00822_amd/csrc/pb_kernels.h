@@ -65,4 +65,38 @@ int launch_bias_act(float *Y, const float *bias, int relu, int rows, int batch, 
 int launch_lstm_pointwise(const float *gates, const float *bias, const float *c_prev, int H, int batch, float *h_out,
                           float *c_out, hipStream_t st);
 
+// pb_gated.hip: H[n][r] = act(pre[n][r]) pre[n][units + r]
+int launch_gated(const float *pre, int units, int gate, int batch, float *H, hipStream_t st);
+
+// pb_grad.hip: dX = dY W through the packed matrix (tiled layouts).  With `gated`, dY are the gradients of the pre-activations [g; u] of
+// H = act(g) u, which the call works out from dH and leaves in `dpre`.
+struct GatedSource {
+    const float *pre, *dH;
+    float *dpre;
+    int gate;
+};
+size_t grad_workspace_bytes(const Layout &L, int batch);
+int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, int bits_used, const float *dY, const GatedSource *gated,
+                int batch, float *dX, void *workspace, hipStream_t st);
+
+// pb_adapters.hip: low-rank adapters beside a layer of rows x cols.  The plan carves the workspace up for a batch.
+struct AdapterPlan {
+    int items;             // tiles of up to sixteen vectors of one adapter, at most
+    int ranks;             // rank tiles of sixteen
+    int slices;            // parts of the sums of u and t
+    size_t items_off, counts_off, starts_off, u_off, t_off, bytes;
+};
+AdapterPlan adapter_plan(const Layout &L, const pb_adapters &ad, int batch, bool indexed);
+// The order of the vectors (by adapter) and its tiles; nothing to do without an index
+int launch_adapter_order(const AdapterPlan &p, const pb_adapters &ad, const int32_t *index, int batch, void *workspace, hipStream_t st);
+// u = A_k x (and t = scale_k B_k^T dY, if dY is given) of the ordered vectors, in parts
+int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, bool indexed, const float *X, const float *dY, int batch,
+                        void *workspace, hipStream_t st);
+// Y += scale_k B_k u
+int launch_adapter_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, bool indexed, int batch, float *Y, void *workspace,
+                      hipStream_t st);
+// dX += A_k^T t (if dX is given), dA_k = sum t x^T, dB_k = scale_k sum dy u^T (where given)
+int launch_adapter_grads(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, bool indexed, const float *X, const float *dY, int batch,
+                         float *dX, float *dA, float *dB, void *workspace, hipStream_t st);
+
 }  // namespace pb

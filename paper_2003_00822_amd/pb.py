@@ -11,6 +11,7 @@ is not built, or was built for another torch or Python; a call then takes 6 to 8
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import importlib
 import os
@@ -32,17 +33,28 @@ PB_LAYOUT_TILE16_V1 = 0x50420002     # matrix-core kernel (what pb_desc_init pic
 PB_LAYOUT_TILE16_GATES_V1 = 0x50420003   # the same with the four gate rows of an LSTM unit in one row tile
 PB_LAYOUT_TILE16_PAIRS_V1 = 0x50420004   # the same with two bitlayers per word as base-4 digits (for serving batches)
 PB_ACT_NONE, PB_ACT_RELU = 0, 1
+PB_GATE_SIGMOID, PB_GATE_SILU, PB_GATE_GELU, PB_GATE_RELU = 0, 1, 2, 3
+PB_TYPE_F32, PB_TYPE_BF16, PB_TYPE_F16 = 0, 1, 2
+PB_MAX_ADAPTERS = 4096
+PB_MAX_RANK = 256
 PB_QUANT_SYMMETRIC, PB_QUANT_RANGE, PB_QUANT_SIGN, PB_QUANT_CLIP_SEARCH = 0, 1, 2, 3
 
 EXPORTS = [
     "pb_desc_init", "pb_desc_init_layout", "pb_quantize_pack_desc", "pb_quantize_pack_mode", "pb_packed_bytes", "pb_workspace_bytes", "pb_quantize_pack", "pb_unpack", "pb_matmul",
     "pb_matmul_static", "pb_matmul_bias_act", "pb_matmul_acc", "pb_matmul_acc_pairs", "pb_act_prep", "pb_matmul_prepared", "pb_fixed_point", "pb_lstm_cell", "pb_strerror", "pb_last_hip_error",
+    "pb_gated_linear", "pb_grad_workspace_bytes", "pb_matmul_grad", "pb_gated_linear_grad", "pb_adapters_workspace_bytes", "pb_matmul_adapters",
+    "pb_matmul_adapters_grad",
 ]
 
 
 class pb_desc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("bits", ctypes.c_int32),
                 ("frac_bits", ctypes.c_int32), ("act_bits", ctypes.c_int32), ("layout", ctypes.c_uint32)]
+
+
+class pb_adapters(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int32), ("rank", ctypes.c_int32), ("type", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
 
 
 class PbError(RuntimeError):
@@ -55,6 +67,7 @@ _lib = None
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _D = ctypes.POINTER(pb_desc)
+_A = ctypes.POINTER(pb_adapters)
 
 
 def lib():
@@ -100,13 +113,28 @@ def lib():
         L.pb_fixed_point.restype = _I
         L.pb_lstm_cell.argtypes = [_P, _P, _D, _I, _P, _I, _P, _P, _P, _P, _P, _I, _P, _P]
         L.pb_lstm_cell.restype = _I
+        L.pb_gated_linear.argtypes = [_P, _P, _D, _I, _P, _I, _P, _I, _P, _P, _P, _P]
+        L.pb_gated_linear.restype = _I
+        L.pb_grad_workspace_bytes.argtypes = [_D, _I]
+        L.pb_grad_workspace_bytes.restype = ctypes.c_size_t
+        L.pb_matmul_grad.argtypes = [_P, _P, _D, _I, _P, _I, _P, _P, _P]
+        L.pb_matmul_grad.restype = _I
+        L.pb_gated_linear_grad.argtypes = [_P, _P, _D, _I, _P, _P, _I, _I, _P, _P, _P, _P]
+        L.pb_gated_linear_grad.restype = _I
+        L.pb_adapters_workspace_bytes.argtypes = [_D, _A, _I]
+        L.pb_adapters_workspace_bytes.restype = ctypes.c_size_t
+        L.pb_matmul_adapters.argtypes = [_P, _P, _D, _I, _P, _I, _A, _P, _P, _P, _P, _P]
+        L.pb_matmul_adapters.restype = _I
+        L.pb_matmul_adapters_grad.argtypes = [_P, _P, _D, _I, _P, _P, _I, _A, _P, _P, _P, _P, _P, _P]
+        L.pb_matmul_adapters_grad.restype = _I
         L.pb_strerror.argtypes = [_I]
         L.pb_strerror.restype = ctypes.c_char_p
         L.pb_last_hip_error.argtypes = []
         L.pb_last_hip_error.restype = _I
         binding, why_not = _use_binding()   # (once more: it may have been built since this module was imported)
         if binding is not None:
-            binding.bind(pb_desc, PbError, {n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in _NATIVE})
+            binding.bind(pb_desc, pb_adapters, PbError,
+                         {n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in _NATIVE + _NATIVE_OPERATORS})
         else:
             warnings.warn("calls go through ctypes, 6 to 8 us slower each: %s (python -m paper_2003_00822_amd.build)"
                           % why_not, RuntimeWarning, stacklevel=2)
@@ -259,6 +287,77 @@ def pb_lstm_cell(packed, scales, d, bits_used, x_t, input_size, h_prev, c_prev, 
                               _ptr(workspace, torch.uint8, "workspace"), _stream(stream)), "pb_lstm_cell")
 
 
+def pb_grad_workspace_bytes(d: pb_desc, batch: int) -> int:
+    return int(lib().pb_grad_workspace_bytes(ctypes.byref(d), batch))
+
+
+def pb_adapters_workspace_bytes(d: pb_desc, adapters: pb_adapters, batch: int) -> int:
+    return int(lib().pb_adapters_workspace_bytes(ctypes.byref(d), ctypes.byref(adapters), batch))
+
+
+def pb_gated_linear(packed, scales, d, bits_used, X, batch, bias, gate, H, pre, workspace, stream=None):
+    _check(lib().pb_gated_linear(_ptr(packed, torch.uint8, "packed"), _ptr(scales, torch.float32, "scales"), ctypes.byref(d), bits_used,
+                                 _ptr(X, torch.float32, "X"), batch, _ptr(bias, torch.float32, "bias"), gate,
+                                 _ptr(H, torch.float32, "H"), _ptr(pre, torch.float32, "pre"),
+                                 _ptr(workspace, torch.uint8, "workspace"), _stream(stream)), "pb_gated_linear")
+
+
+def pb_matmul_grad(packed, scales, d, bits_used, dY, batch, dX, workspace, stream=None):
+    _check(lib().pb_matmul_grad(_ptr(packed, torch.uint8, "packed"), _ptr(scales, torch.float32, "scales"), ctypes.byref(d), bits_used,
+                                _ptr(dY, torch.float32, "dY"), batch, _ptr(dX, torch.float32, "dX"),
+                                _ptr(workspace, torch.uint8, "workspace"), _stream(stream)), "pb_matmul_grad")
+
+
+def pb_gated_linear_grad(packed, scales, d, bits_used, pre, dH, batch, gate, dpre, dX, workspace, stream=None):
+    _check(lib().pb_gated_linear_grad(_ptr(packed, torch.uint8, "packed"), _ptr(scales, torch.float32, "scales"), ctypes.byref(d), bits_used,
+                                      _ptr(pre, torch.float32, "pre"), _ptr(dH, torch.float32, "dH"), batch, gate,
+                                      _ptr(dpre, torch.float32, "dpre"), _ptr(dX, torch.float32, "dX"),
+                                      _ptr(workspace, torch.uint8, "workspace"), _stream(stream)), "pb_gated_linear_grad")
+
+
+def pb_matmul_adapters(packed, scales, d, bits_used, X, batch, adapters, index, bias, Y, workspace, stream=None):
+    _check(lib().pb_matmul_adapters(_ptr(packed, torch.uint8, "packed"), _ptr(scales, torch.float32, "scales"), ctypes.byref(d), bits_used,
+                                    _ptr(X, torch.float32, "X"), batch, ctypes.byref(adapters), _ptr(index, torch.int32, "index"),
+                                    _ptr(bias, torch.float32, "bias"), _ptr(Y, torch.float32, "Y"),
+                                    _ptr(workspace, torch.uint8, "workspace"), _stream(stream)), "pb_matmul_adapters")
+
+
+def pb_matmul_adapters_grad(packed, scales, d, bits_used, X, dY, batch, adapters, index, dX, dA, dB, workspace, stream=None):
+    _check(lib().pb_matmul_adapters_grad(_ptr(packed, torch.uint8, "packed"), _ptr(scales, torch.float32, "scales"), ctypes.byref(d),
+                                         bits_used, _ptr(X, torch.float32, "X"), _ptr(dY, torch.float32, "dY"), batch,
+                                         ctypes.byref(adapters), _ptr(index, torch.int32, "index"), _ptr(dX, torch.float32, "dX"),
+                                         _ptr(dA, torch.float32, "dA"), _ptr(dB, torch.float32, "dB"),
+                                         _ptr(workspace, torch.uint8, "workspace"), _stream(stream)), "pb_matmul_adapters_grad")
+
+
+_TYPES = {torch.float32: PB_TYPE_F32, torch.bfloat16: PB_TYPE_BF16, torch.float16: PB_TYPE_F16}
+
+
+class Adapters:
+    """Low-rank adapters of one layer, of many requests: adapter k adds scale[k] B[k] A[k] to its matrix.  A [count, rank, cols] and B [count,
+    rows, rank] of one type (float32, bfloat16, float16), scale [count] float32 or None for 1."""
+
+    def __init__(self, A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor | None = None):
+        if A.dtype not in _TYPES or B.dtype != A.dtype:
+            raise TypeError("A and B must both be float32, bfloat16 or float16, got %s and %s" % (A.dtype, B.dtype))
+        if A.dim() != 3 or B.dim() != 3 or A.shape[0] != B.shape[0] or A.shape[1] != B.shape[2]:
+            raise ValueError("A [count, rank, cols] and B [count, rows, rank], got %s and %s" % (tuple(A.shape), tuple(B.shape)))
+        if scale is not None and scale.shape != (A.shape[0],):
+            raise ValueError("scale [count], got %s" % (tuple(scale.shape),))
+        self.A, self.B, self.scale = A, B, scale
+        self.count, self.rank, self.cols = A.shape
+        self.rows = B.shape[1]
+        self.desc()
+
+    def desc(self) -> pb_adapters:
+        """The tensors as they are now (an optimizer may have put others in their place)."""
+        A, B = self.A, self.B
+        if A.dtype not in _TYPES or A.shape != (self.count, self.rank, self.cols) or B.shape != (self.count, self.rows, self.rank):
+            raise ValueError("A or B has another type or shape than it had")
+        return pb_adapters(self.count, self.rank, _TYPES[A.dtype], 0, _ptr(A, None, "A"), _ptr(B, A.dtype, "B"),
+                           _ptr(self.scale, torch.float32, "scale"))
+
+
 class PackedLinear:
     """Convenience holder: one quantized, packed weight matrix with its scales and a workspace."""
 
@@ -308,6 +407,101 @@ class PackedLinear:
         pb_matmul_acc_pairs(self.packed, self.desc, m, X, batch, A, torch.empty_like(self.workspace))
         return A
 
+    # The calls below have workspaces of their own: they take any stream and thread, and a captured graph keeps its own.
+
+    def gated(self, X: torch.Tensor, gate: int = PB_GATE_SILU, bits_used: int | None = None, bias: torch.Tensor | None = None,
+              keep: bool = False):
+        """H = act(g) u with [g; u] = W x + bias: the block's two projections packed as one matrix, gate rows first.  With `keep` also the
+        pre-activations [g; u], for gated_grad."""
+        X = self._vectors(X, self.cols, "X")
+        n = X.shape[0]
+        with self._here(X, bias):
+            H = torch.empty((n, self.rows // 2), dtype=torch.float32, device=X.device)
+            pre = torch.empty((n, self.rows), dtype=torch.float32, device=X.device) if keep else None
+            self._sized(bias, "bias", (self.rows,))
+            pb_gated_linear(self.packed, self.scales, self.desc, self.bits if bits_used is None else bits_used, X, n, bias, gate, H, pre,
+                            self._work(pb_workspace_bytes(self.desc, n)))
+        return (H, pre) if keep else H
+
+    def gated_grad(self, pre: torch.Tensor, dH: torch.Tensor, gate: int = PB_GATE_SILU, bits_used: int | None = None):
+        """(dX, dpre) of `gated`, from the pre-activations that it kept."""
+        pre, dH = self._vectors(pre, self.rows, "pre"), self._vectors(dH, self.rows // 2, "dH")
+        n = pre.shape[0]
+        self._sized(dH, "dH", (n, self.rows // 2))
+        with self._here(pre, dH):
+            dX = torch.empty((n, self.cols), dtype=torch.float32, device=pre.device)
+            dpre = torch.empty_like(pre)
+            pb_gated_linear_grad(self.packed, self.scales, self.desc, self.bits if bits_used is None else bits_used, pre, dH, n, gate, dpre, dX,
+                                 self._work(pb_grad_workspace_bytes(self.desc, n)))
+        return dX, dpre
+
+    def grad(self, dY: torch.Tensor, bits_used: int | None = None):
+        """dX = dY W: the gradient of the layer's activations, through the first `bits_used` bitlayers."""
+        dY = self._vectors(dY, self.rows, "dY")
+        n = dY.shape[0]
+        with self._here(dY):
+            dX = torch.empty((n, self.cols), dtype=torch.float32, device=dY.device)
+            pb_matmul_grad(self.packed, self.scales, self.desc, self.bits if bits_used is None else bits_used, dY, n, dX,
+                           self._work(pb_grad_workspace_bytes(self.desc, n)))
+        return dX
+
+    def adapted(self, X: torch.Tensor, adapters: Adapters, index: torch.Tensor | None, bits_used: int | None = None,
+                bias: torch.Tensor | None = None):
+        """W x + bias + scale_k B_k A_k x with k = index[n] (int32; outside [0, count): no adapter; None: adapter 0 for all)."""
+        X = self._vectors(X, self.cols, "X")
+        n = X.shape[0]
+        self._sized(index, "index", (n,))
+        self._sized(bias, "bias", (self.rows,))
+        with self._here(X, index, bias, adapters.A):
+            desc = self._desc_of(adapters)
+            Y = torch.empty((n, self.rows), dtype=torch.float32, device=X.device)
+            pb_matmul_adapters(self.packed, self.scales, self.desc, self.bits if bits_used is None else bits_used, X, n, desc, index, bias, Y,
+                               self._work(pb_adapters_workspace_bytes(self.desc, desc, n)))
+        return Y
+
+    def adapted_grad(self, X: torch.Tensor, dY: torch.Tensor, adapters: Adapters, index: torch.Tensor | None, bits_used: int | None = None,
+                     inputs: bool = True):
+        """(dX, dA, dB) of `adapted`, all fp32; dX is None without `inputs`."""
+        X, dY = self._vectors(X, self.cols, "X"), self._vectors(dY, self.rows, "dY")
+        n = X.shape[0]
+        self._sized(dY, "dY", (n, self.rows))
+        self._sized(index, "index", (n,))
+        with self._here(X, dY, index, adapters.A):
+            desc = self._desc_of(adapters)
+            dX = torch.empty((n, self.cols), dtype=torch.float32, device=X.device) if inputs else None
+            dA = torch.empty(adapters.A.shape, dtype=torch.float32, device=X.device)
+            dB = torch.empty(adapters.B.shape, dtype=torch.float32, device=X.device)
+            pb_matmul_adapters_grad(self.packed, self.scales, self.desc, self.bits if bits_used is None else bits_used, X, dY, n, desc, index,
+                                    dX, dA, dB, self._work(pb_adapters_workspace_bytes(self.desc, desc, n)))
+        return dX, dA, dB
+
+    def _vectors(self, t, length, name):
+        if t.dim() < 1 or t.shape[-1] != length:
+            raise ValueError("%s must have vectors of %d values, got %s" % (name, length, tuple(t.shape)))
+        return t if t.dim() == 2 else t.reshape(-1, length)
+
+    @staticmethod
+    def _sized(t, name, shape):
+        if t is not None and t.shape != shape:
+            raise ValueError("%s must have the shape %s, got %s" % (name, shape, tuple(t.shape)))
+
+    def _desc_of(self, adapters):
+        if (adapters.rows, adapters.cols) != (self.rows, self.cols):
+            raise ValueError("adapters of a layer %d x %d, the layer is %d x %d" % (adapters.rows, adapters.cols, self.rows, self.cols))
+        return adapters.desc()
+
+    def _here(self, *tensors):
+        """The layer's device as the current one; all tensors are on it."""
+        device = self.packed.device
+        for t in tensors:
+            if t is not None and t.device != device:
+                raise ValueError("a tensor is on %s, the layer on %s" % (t.device, device))
+        return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+    def _work(self, size):
+        # (a size of 0: the call is refused, and says why)
+        return torch.empty(max(size, 16), dtype=torch.uint8, device=self.packed.device)
+
     def unpack(self):
         q = torch.empty((self.rows, self.cols), dtype=torch.int32, device=self.packed.device)
         pb_unpack(self.packed, self.desc, q)
@@ -318,8 +512,9 @@ class PackedLinear:
 _NATIVE = ["pb_quantize_pack", "pb_quantize_pack_desc", "pb_quantize_pack_mode", "pb_unpack", "pb_matmul",
            "pb_matmul_static", "pb_matmul_bias_act", "pb_matmul_acc", "pb_matmul_acc_pairs", "pb_act_prep",
            "pb_matmul_prepared", "pb_fixed_point", "pb_lstm_cell"]
+_NATIVE_OPERATORS = ["pb_gated_linear", "pb_matmul_grad", "pb_gated_linear_grad", "pb_matmul_adapters", "pb_matmul_adapters_grad"]
 _linear = PackedLinear._call_checked
-_PYTHON = {**{n: globals()[n] for n in _NATIVE}, "linear": _linear}
+_PYTHON = {**{n: globals()[n] for n in _NATIVE + _NATIVE_OPERATORS}, "linear": _linear}
 
 
 def _use_binding():
@@ -332,8 +527,10 @@ def _use_binding():
     here = "%s %s" % (torch.__version__, sys.implementation.cache_tag)
     if getattr(binding, "BUILT_FOR", None) != here:   # (it takes tensors apart by torch's headers)
         return None, "the native binding is built for %s, not for %s" % (getattr(binding, "BUILT_FOR", "?"), here)
+    if not all(hasattr(binding, n) for n in _NATIVE + _NATIVE_OPERATORS):
+        return None, "the native binding is built from other sources"
     binding.set_slow(_PYTHON)
-    globals().update({n: getattr(binding, n) for n in _NATIVE})
+    globals().update({n: getattr(binding, n) for n in _NATIVE + _NATIVE_OPERATORS})
     globals()["_linear"] = binding.linear
     return binding, None
 
