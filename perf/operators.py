@@ -130,7 +130,9 @@ def prepare(case, seed):
         from paper_2003_00822_amd import pb
         # a gated layer of an even number of units has the layout that the block's single launch takes
         layout = pb.PB_LAYOUT_TILE16_GATES_V1 if case.get("units", 1) % 2 == 0 else None
-        s["layer"] = pb.PackedLinear(W, case["bits"], max_batch=case["batch"], layout=layout)
+        # (packed from the quantized matrix: a weight half way between two codes must not depend on how the step was rounded)
+        codes, step = _codes(W, case["bits"], case["bits"])
+        s["layer"] = pb.PackedLinear(codes * step, case["bits"], max_batch=case["batch"], layout=layout)
         if "A" in s:
             s["adapters"] = pb.Adapters(s["A"], s["B"], s["scale"])
         if "gate" in case:
