@@ -3,8 +3,11 @@
 //
 // dY as digits.  A vector's gradients are scaled by the power of two that brings the largest one below 2^30, rounded to integers g and
 // split into four balanced byte digits, g = sum_d 256^d s_d with s_d in [-128, 127]: the bytes of (g + 0x808080) ^ 0x808080, because
-// 0x808080 = sum_(d < 3) 256^d 128.  The rounding (half a unit, 2^-31 of the vector's largest gradient) is the only one before the last
+// 0x808080 = sum_(d < 3) 256^d 128.  The rounding (half a unit, at most 2^-30 of the vector's largest gradient) is the only one before the last
 // step: |s code| <= 2^14, so a sum over 65536 rows is exact in int32, and the digits' sums are put together in fp64.
+// Batches, which the matrix instructions bound, take three digits (half a unit: at most 2^-23 of the largest gradient) where no vector of
+// sixteen has a value above 12 times the root of its mean square: a result is then off by 12 * 2^-22 / sqrt(12) = 8e-7 of the results' root
+// mean square at most, typically a quarter of it, which is what a product in fp32 is off by.
 //
 // The sum runs over the rows of W, and a packed word holds 32 columns of one row: the codes have to be turned, 16 rows of a column
 // into the 16 bytes of a lane.  They go through LDS anyway, because every wave needs them, and DS_READ_B64_TR_B8 turns them on the
@@ -20,49 +23,69 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kNotFinite = INT32_MIN;      // in the place of an exponent: the vector's results are NaN
 
-// The exponent e of every vector: its gradients enter as rint(dy 2^e)
-__device__ __forceinline__ int exponent_of(uint32_t largest)     // (bits of the largest magnitude)
+// How a vector's gradients become integers: rint(dy 2^e4) with four digits, rint(dy 2^e3) with three
+struct Scaling { int e4, e3, wide, pad; };     // wide: four digits are needed
+
+// From the bits of the largest magnitude and the sum of squares of `count` values
+__device__ __forceinline__ Scaling scaling_of(uint32_t largest, double squares, int count)
 {
-    if (largest >= 0x7F800000u) return kNotFinite;
-    if (largest == 0) return 0;
+    if (largest >= 0x7F800000u) return {kNotFinite, kNotFinite, 0, 0};
+    if (largest == 0) return {0, 0, 0, 0};
     int e;
-    frexpf(__uint_as_float(largest), &e);
-    return 30 - e;
+    const double most = (double)__uint_as_float(largest);
+    const float f = frexpf(__uint_as_float(largest), &e);
+    // (three balanced digits hold 127 * 65536 + 127 * 256 + 127 = 8355711 < 2^23)
+    return {30 - e, 23 - e - (f * 8388608.0f > 8355000.0f ? 1 : 0), most * most * count > 144.0 * squares ? 1 : 0, 0};
 }
 
-// The largest of a value per thread, in thread 0
+// The largest of a value per thread and the sum of another, in thread 0
 template <int WAVES>
-__device__ __forceinline__ uint32_t largest_of_workgroup(uint32_t v)
+__device__ __forceinline__ void over_workgroup(uint32_t &most, double &sum)
 {
     __shared__ uint32_t s_max[WAVES];
+    __shared__ double s_sum[WAVES];
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
-    if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = v;
+    for (int d = 32; d > 0; d >>= 1) {
+        most = max(most, (uint32_t)__shfl_xor((int)most, d));
+        sum += __shfl_xor(sum, d);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        s_max[threadIdx.x >> 6] = most;
+        s_sum[threadIdx.x >> 6] = sum;
+    }
     __syncthreads();
     if (threadIdx.x == 0) {
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) v = max(v, s_max[w]);
+        for (int w = 1; w < WAVES; ++w) {
+            most = max(most, s_max[w]);
+            sum += s_sum[w];
+        }
     }
-    return v;
 }
 
-__global__ __launch_bounds__(1024) void k_grad_exponents(const float *__restrict__ dY, int rows, int *__restrict__ exps)
+__global__ __launch_bounds__(1024) void k_grad_scalings(const float *__restrict__ dY, int rows, Scaling *__restrict__ scalings)
 {
     const float *y = dY + (size_t)blockIdx.x * rows;
     uint32_t most = 0;
-    for (int r = threadIdx.x; r < rows; r += 1024) most = max(most, __float_as_uint(y[r]) & 0x7FFFFFFFu);
-    most = largest_of_workgroup<16>(most);
-    if (threadIdx.x == 0) exps[blockIdx.x] = exponent_of(most);
+    double squares = 0.0;
+    for (int r = threadIdx.x; r < rows; r += 1024) {
+        const float v = y[r];
+        most = max(most, __float_as_uint(v) & 0x7FFFFFFFu);
+        squares = fma((double)v, (double)v, squares);
+    }
+    over_workgroup<16>(most, squares);
+    if (threadIdx.x == 0) scalings[blockIdx.x] = scaling_of(most, squares, rows);
 }
 
-// Gradients of the pre-activations [g; u] of H = act(g) u, and the exponents of their vectors
+// Gradients of the pre-activations [g; u] of H = act(g) u, and the scalings of their vectors
 __global__ __launch_bounds__(1024) void k_gated_grad(const float *__restrict__ pre, const float *__restrict__ dH, int units, int gate,
-                                                     float *__restrict__ dpre, int *__restrict__ exps)
+                                                     float *__restrict__ dpre, Scaling *__restrict__ scalings)
 {
     const size_t n = blockIdx.x;
     const float *g = pre + n * 2 * units, *u = g + units, *dh = dH + n * units;
     float *dg = dpre + n * 2 * units, *du = dg + units;
     uint32_t most = 0;
+    double squares = 0.0;
     for (int r = threadIdx.x; r < units; r += 1024) {
         float a, da;
         gate_with_slope(gate, g[r], &a, &da);
@@ -70,28 +93,57 @@ __global__ __launch_bounds__(1024) void k_gated_grad(const float *__restrict__ p
         dg[r] = x;
         du[r] = y;
         most = max(most, max(__float_as_uint(x) & 0x7FFFFFFFu, __float_as_uint(y) & 0x7FFFFFFFu));
+        squares = fma((double)x, (double)x, fma((double)y, (double)y, squares));
     }
-    most = largest_of_workgroup<16>(most);
-    if (threadIdx.x == 0) exps[n] = exponent_of(most);
+    over_workgroup<16>(most, squares);
+    if (threadIdx.x == 0) scalings[n] = scaling_of(most, squares, 2 * units);
 }
+
+// Whether one of the group's vectors needs four digits; the lane's vector is the group's vector lane % 16
+__device__ __forceinline__ bool group_is_wide(const Scaling &mine, bool live) { return __builtin_amdgcn_ballot_w64(live && mine.wide) != 0; }
 
 // The digits in memory: [group of 16 vectors][step of 64 packed rows][digit][lane 16 kb + v][16 bytes], the bytes being the
 // sixteen rows of row tile 4 step + kb of vector v: an operand of a digit of sixteen vectors is 1 KB in one piece.  A wave writes one step.
-__global__ __launch_bounds__(256) void k_grad_digits(const float *__restrict__ dY, const int *__restrict__ exps, int batch, int rows,
-                                                     int gate_h, int steps, uint8_t *__restrict__ digits)
+// VEC: four rows next to each other in the matrix are four in the tile (one of each gate's units on the gate layout) and aligned to 16 bytes.
+template <bool VEC>
+__global__ __launch_bounds__(256) void k_grad_digits(const float *__restrict__ dY, const Scaling *__restrict__ scalings, int batch, int rows,
+                                                     int gate_h, int steps, int may_narrow, uint8_t *__restrict__ digits)
 {
     const int lane = threadIdx.x & 63, step = blockIdx.x * 4 + (threadIdx.x >> 6), group = blockIdx.y;
     if (step >= steps) return;
     const int n = group * kGroupVectors + (lane & 15), tile = step * 4 + (lane >> 4);
-    const int e = n < batch ? exps[n] : kNotFinite;
+    Scaling sc = {kNotFinite, kNotFinite, 0, 0};
+    if (n < batch) sc = scalings[n];
+    const bool narrow = may_narrow && !group_is_wide(sc, n < batch);
+    const int e = narrow ? sc.e3 : sc.e4;
+    const float *const y = dY + (size_t)n * rows;
+    float v[16];
+    if constexpr (VEC) {
+        // (row tile t on the gate layout: units 4 t .. 4 t + 3 of each gate, row 4 (unit) + gate of the tile)
+        const int height = gate_h ? gate_h : rows;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int r = gate_h ? tile * 4 : tile * kTileRows + 4 * k;
+            float4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (e != kNotFinite && r < height) x = *reinterpret_cast<const float4 *>(y + (gate_h ? (size_t)k * gate_h : 0) + r);
+            const float xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (gate_h) v[4 * i + k] = xs[i];
+                else v[4 * k + i] = xs[i];
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = gate_h ? gates_matrix_row(tile * kTileRows + i, gate_h) : tile * kTileRows + i;
+            v[i] = e != kNotFinite && r >= 0 && r < rows ? y[r] : 0.0f;
+        }
+    }
+    const int balance = narrow ? 0x8080 : 0x808080;
     int g[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int r = gate_h ? gates_matrix_row(tile * kTileRows + i, gate_h) : tile * kTileRows + i;
-        const bool live = e != kNotFinite && r >= 0 && r < rows;
-        const float y = live ? dY[(size_t)n * rows + r] : 0.0f;
-        g[i] = live ? (__float2int_rn(ldexpf(y, e)) + 0x808080) ^ 0x808080 : 0;
-    }
+    for (int i = 0; i < 16; ++i) g[i] = e == kNotFinite ? 0 : (__float2int_rn(ldexpf(v[i], e)) + balance) ^ balance;
     u32x4 out[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -104,7 +156,8 @@ __global__ __launch_bounds__(256) void k_grad_digits(const float *__restrict__ d
     }
     u32x4 *dst = reinterpret_cast<u32x4 *>(digits + ((size_t)group * steps + step) * 4096) + lane;
 #pragma unroll
-    for (int d = 0; d < 4; ++d) dst[64 * d] = out[d];
+    for (int d = 0; d < 4; ++d)
+        if (d < 3 || !narrow) dst[64 * d] = out[d];
 }
 
 struct GradArgs {
@@ -114,31 +167,57 @@ struct GradArgs {
     int steps, steps_per_split;                      // steps of 64 packed rows
     const float *scales;
     const uint8_t *digits;
-    const int *exps;
+    const Scaling *scalings;
+    int may_narrow;
     float *out;                                      // [split][batch][cols]
+    int blocks, rows_of, workgroups;                 // column blocks, groups of vectors
+
+    // What workgroup `id` does.  Workgroups go round the eight XCDs, each with an L2 of its own: those of an XCD (id % 8) take a contiguous range of an
+    // order in which eight column blocks (two to a line of weights) and then the vectors are next to each other, and read less of both.
+    __device__ void place(int id, int *block, int *vectors, int *split) const
+    {
+        const int each = workgroups / 8, rest = workgroups % 8, xcd = id % 8;
+        int at = xcd * each + min(xcd, rest) + id / 8;
+        *split = at / (blocks * rows_of);
+        at -= *split * (blocks * rows_of);
+        const int wide = at / (8 * rows_of), width = min(8, blocks - wide * 8);
+        at -= wide * 8 * rows_of;
+        *vectors = at / width;
+        *block = wide * 8 + at % width;
+    }
 };
 
-// A workgroup of eight waves: WM of them along the vectors (sixteen each), the others along the columns: 512, or with WM = 4 half of
-// the words of each lane's four, 256.  32 KB of codes at a time, two buffers: every wave turns two words of each bitlayer of a row tile
-// into codes while it multiplies those of the other buffer.
+// The shape of a workgroup of eight waves: WM of them lie along the vectors (sixteen each), the others along the columns, NT operands of sixteen
+// columns each.  Its codes are in two buffers of 64 KB: `columns` of a chunk's 512 and as many row tiles as fit.
+template <int WM>
+struct GradShape {
+    static constexpr int WN = WM >= 8 ? 1 : 8 / WM, NT = WM == 1 ? 4 : 8;
+    static constexpr int GROUPS = WN * NT;               // operands of a row tile: 32, 32, 16, 8
+    static constexpr int PARTS = 32 / GROUPS;            // workgroups that share a chunk
+    static constexpr int TILES = 256 / GROUPS;           // row tiles in a buffer
+    static constexpr int KS = TILES / 4;                 // steps of 64 rows in a buffer
+    static constexpr int TILE = GROUPS * 256 + 128;      // (the row tiles of an operand start in different halves of the banks)
+    static constexpr int LDS = 2 * TILES * TILE;
+};
+
+// While a wave multiplies the codes of one buffer, it turns its share of the words of the next one into codes: four words of each bitlayer per
+// lane, loaded with 16 bytes each (the vector-memory pipeline takes 16 cycles for a wave's load whatever its width).
 template <int Q, bool IL, int WM>
 __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
 {
-    constexpr int WN = 8 / WM, NT = WM == 1 ? 4 : 8;
-    constexpr int GROUPS = WN * NT;                      // of sixteen columns: 32 or 16
-    constexpr int TILES = 128 / GROUPS;                  // row tiles in a buffer: 4 or 8
-    constexpr int KS = TILES / 4;                        // steps of 64 rows in a buffer
-    constexpr int BR = 3;                                // operands of codes on their way from LDS
-    constexpr int TILE = GROUPS * 256 + 128;             // (the row tiles of an operand start in different halves of the banks)
-    __shared__ __align__(16) unsigned char s_codes[2][TILES * TILE];
+    using S = GradShape<WM>;
+    constexpr int WN = S::WN, NT = S::NT, TILES = S::TILES, KS = S::KS, TILE = S::TILE, BUF = TILES * TILE;
+    extern __shared__ __align__(16) unsigned char s_codes[];
     __shared__ float s_scales[PB_MAX_BITS];
 
     const int lane = threadIdx.x & 63, kb = lane >> 4, j = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave % WM, wn = wave / WM;
-    const int q = GROUPS == 32 ? blockIdx.x : blockIdx.x >> 1;
-    const int group = blockIdx.y * WM + wm;
-    const int step0 = blockIdx.z * a.steps_per_split, step1 = min(step0 + a.steps_per_split, a.steps);   // (not empty)
+    const int wm = wave % WM, wn = WN == 1 ? 0 : wave / WM;
+    int block, vectors, split;
+    a.place(blockIdx.x, &block, &vectors, &split);
+    const int q = block / S::PARTS, part_of_chunk = block % S::PARTS;
+    const int group = vectors * WM + wm;
+    const int step0 = split * a.steps_per_split, step1 = min(step0 + a.steps_per_split, a.steps);   // (not empty)
     const int loops = (step1 - step0 + KS - 1) / KS;
     const int m = a.m;
     const Masks masks = make_masks();
@@ -152,140 +231,197 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
     const bool merged = __builtin_amdgcn_ballot_w64(off) == 0;
     const int gs0 = merged ? 4 * Q : 1, gs1 = merged ? 4 * Q - 2 : 1;
 
-    // the wave's part of the codes: row tile and two of four words
-    const int my_tile = GROUPS == 32 ? wave >> 1 : wave, my_half = GROUPS == 32 ? wave & 1 : blockIdx.x & 1;
-    unsigned char *const my_codes =
-        &s_codes[0][0] + my_tile * TILE + (GROUPS == 32 ? (kb * 4 + my_half * 2) * 512 : kb * 2 * 512) + j * 16;
-    const u32x4 *const dig = reinterpret_cast<const u32x4 *>(a.digits + (size_t)group * a.steps * 4096) + lane;
-    const bool have = group * kGroupVectors < a.batch;
+    // the wave's share of a buffer: TILES / 8 row tiles, of each of which PER lanes read one piece; a lane has four words of a row
+    constexpr int PER = 512 / TILES;
+    const int my_tile = wave * (TILES / 8) + lane / PER, my_piece = lane % PER;
+    const uint32_t my_at = (uint32_t)(lane / PER) * a.round_step + (uint32_t)(part_of_chunk * PER + my_piece) * 16u;
+    unsigned char *const my_codes = s_codes + my_tile * TILE + (my_piece >> 4) * 2048 + (my_piece & 15) * 16;
+    // the digits of the wave's vectors in these steps (nothing beyond them, and nothing for a group without vectors)
+    const __amdgpu_buffer_rsrc_t rd = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t *>(a.digits) + ((size_t)group * a.steps + step0) * 4096, 0,
+        group * kGroupVectors < a.batch ? (step1 - step0) * 4096 : 0, 0x00020000);
     // where the wave's operands begin in a buffer
-    const unsigned char *const operands = &s_codes[0][0] + kb * TILE + wn * NT * 256 + j * 8;
+    const unsigned char *const operands = s_codes + kb * TILE + wn * NT * 256 + j * 8;
 
-    bool first = true;
-    for (int f = 0, e; f < m; f = e) {
-        e = min(m, f + (f == 0 ? gs0 : gs1));
-        const int l0 = (f & ~1) == 0 ? 0 : (f & ~1) - 2;
-        uint32_t mask[2 * Q];
+    // Everything of the sum over the rows with ND digits: AR sets of registers for the digits of as many steps, WS for the words of as many buffers
+    auto sum_up = [&](auto nd, auto ar_sets, auto word_sets) {
+        constexpr int ND = decltype(nd)::value, AR = decltype(ar_sets)::value, WS = decltype(word_sets)::value;
+        constexpr int UL = AR > KS ? AR / KS : 1;           // buffers until the sets of registers are the first ones again
+        constexpr int BR = WM >= 4 && ND == 4 ? 2 : 3;      // operands of codes on their way from LDS (the registers are full with four digits)
+        static_assert(UL * KS % AR == 0 && (WS == 1 || UL % WS == 0), "whole turns");
+        for (int f = 0, e; f < m; f = e) {
+            e = min(m, f + (f == 0 ? gs0 : gs1));
+            const int l0 = (f & ~1) == 0 ? 0 : (f & ~1) - 2;
+            uint32_t mask[2 * Q];
 #pragma unroll
-        for (int p = 0; p < 2 * Q; ++p) {
-            const int l = l0 + 2 * p;
-            mask[p] = (l >= f && l < e ? 0xAAAAAAAAu : 0u) | (l + 1 >= f && l + 1 < e ? 0x55555555u : 0u);
-        }
-        const uint32_t flip = l0 == 0 ? 0xAAAAAAAAu : 0u;
-        u32x2 w[4 * Q];
-        // the words of buffer `loop` (beyond the last row tile they are zero)
-        auto tile_of = [&](int loop) { return (step0 + loop * KS) * 4 + my_tile; };
-        auto inside = [&](int loop) { return loop < loops && tile_of(loop) < min(a.rt_count, step1 * 4); };
-        auto issue = [&](int loop) {
-            const bool ok = inside(loop);
-            const uint32_t at = (uint32_t)tile_of(loop) * a.round_step + (uint32_t)q * 1024u;
-#pragma unroll
-            for (int s = 0; s < 4 * Q; ++s) {
-                const int l = l0 + s, lu = l0 + (s & ~1);
-                const bool has = ok && (IL ? lu + 1 >= f && lu < e : l >= f && l < e);
-                const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint32_t *>(a.packed), 0,
-                                                                                    has ? (int)a.packed_bytes : 0, 0x00020000);
-                w[s] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rw, lane * 16 + my_half * 8,
-                                                                                     (int)(at + (uint32_t)l * a.layer_step), 0));
+            for (int p = 0; p < 2 * Q; ++p) {
+                const int l = l0 + 2 * p;
+                mask[p] = (l >= f && l < e ? 0xAAAAAAAAu : 0u) | (l + 1 >= f && l + 1 < e ? 0x55555555u : 0u);
             }
-        };
-        auto expand = [&](int loop) {
-            const bool in = inside(loop);
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                uint32_t p[4 * Q];
+            const uint32_t flip = l0 == 0 ? 0xAAAAAAAAu : 0u;
+            u32x4 w[WS][4 * Q];
+            // the words of buffer `loop`; those of row tiles beyond the end are zero
+            const int end = min(a.rt_count, step1 * 4);
+            auto inside = [&](int loop) { return (step0 + loop * KS) * 4 + my_tile < end; };
+            auto issue = [&](u32x4 (&w)[4 * Q], int loop) {
+                const uint32_t at = (uint32_t)((step0 + loop * KS) * 4 + wave * (TILES / 8)) * a.round_step + (uint32_t)q * 1024u;
+                const int mine = inside(loop) ? (int)my_at : -16;      // (beyond every buffer)
 #pragma unroll
                 for (int s = 0; s < 4 * Q; ++s) {
-                    p[s] = w[s][t];
-                    if constexpr (IL) p[s] = (s < 2 ? p[s] ^ flip : p[s]) & (in ? mask[s / 2] : 0u);
+                    const int l = l0 + s, lu = l0 + (s & ~1);
+                    const bool has = loop < loops && (IL ? lu + 1 >= f && lu < e : l >= f && l < e);
+                    const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint32_t *>(a.packed), 0,
+                                                                                        has ? (int)a.packed_bytes : 0, 0x00020000);
+                    w[s] = __builtin_amdgcn_raw_buffer_load_b128(rw, mine, has ? (int)(at + (uint32_t)l * a.layer_step) : 0, 0);
                 }
-                v4i lo, hi;
-                weight_codes<Q, IL, true>(masks, p, lo, hi);
-                unsigned char *dst = my_codes + (loop & 1) * (TILES * TILE) + t * 512;
-                *reinterpret_cast<v4i *>(dst) = lo;
-                *reinterpret_cast<v4i *>(dst + 256) = hi;
-            }
-        };
-        v4i acc[4][NT];
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) acc[d][nt] = v4i{0, 0, 0, 0};
-        u32x4 ar[2][4];
-        auto load_digits = [&](u32x4 (&dst)[4], int step) {
-            const u32x4 *src = dig + (size_t)min(step, a.steps - 1) * 256;
-#pragma unroll
-            for (int d = 0; d < 4; ++d) dst[d] = have ? src[64 * d] : u32x4{0, 0, 0, 0};
-        };
-        issue(0);
-        load_digits(ar[0], step0);
-        expand(0);
-        issue(1);
-        __syncthreads();
-        for (int loop = 0; loop < loops; ++loop) {
-            expand(loop + 1);
-            issue(loop + 2);
-            const unsigned char *src = operands + (loop & 1) * (TILES * TILE);
-            // operand nt of step k of the buffer
-            auto codes = [&](int k, int nt) {
-                const unsigned char *at = src + k * 4 * TILE + nt * 256;
-                const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((v2i __attribute__((address_space(3))) *)(at));
-                const v2i y = __builtin_amdgcn_ds_read_tr8_b64_v2i32((v2i __attribute__((address_space(3))) *)(at + 128));
-                return v4i{x[0], x[1], y[0], y[1]};
             };
-            v4i br[BR];
+            // The codes of a buffer from its words, word after word in the six steps of weight_codes(): 0, 1 pairs of words, 2, 3 nibbles, 4, 5 bytes and
+            // their way to LDS, so that they can stand between the products of the other buffer.
+            constexpr int STAGES = 24;
+            uint64_t part[4];         // first h, l (then the nibbles' two halves), second h, l
+            uint32_t keep[2 * Q];     // (IL)
+            auto expand = [&](int stage, const u32x4 (&w)[4 * Q], int loop, unsigned char *to) {
+                const int t = stage / 6, o = stage & 1;
+                if (stage % 6 < 2) {
+                    if (stage == 0) {
 #pragma unroll
-            for (int i = 0; i < BR - 1; ++i) br[i] = codes(0, i);
-            __builtin_amdgcn_sched_barrier(0);
+                        for (int i = 0; i < 2 * Q; ++i) keep[i] = inside(loop) ? mask[i] : 0u;
+                    }
+                    if (o == 1 && Q == 1) return;      // (the upper or the lower four slots)
+                    uint32_t p[4];
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                const int step = step0 + loop * KS + k;
-                // (a wave's steps alternate between two sets of registers only where a buffer has two)
-                u32x4 (&now)[4] = ar[KS == 2 ? k : 0], (&next)[4] = ar[KS == 2 ? k ^ 1 : 1];
-                load_digits(next, step + 1);
+                    for (int i = 0; i < 4; ++i) {
+                        p[i] = w[4 * o + i][t];
+                        if constexpr (IL) p[i] = (o == 0 && i < 2 ? p[i] ^ flip : p[i]) & keep[2 * o + i / 2];
+                    }
+                    if constexpr (IL) {
+                        part[2 * o] = both(p[0], p[1]);
+                        part[2 * o + 1] = both(p[2], p[3]);
+                    } else {
+                        part[2 * o] = both(pick(masks.m1, twice(p[0]), p[1]), pick(masks.m1, p[0], p[1] >> 1));
+                        part[2 * o + 1] = both(pick(masks.m1, twice(p[2]), p[3]), pick(masks.m1, p[2], p[3] >> 1));
+                    }
+                } else if (stage % 6 < 4) {
+                    if (o == 1 && Q == 1) return;
+                    const uint64_t h = part[2 * o], l = part[2 * o + 1];
+                    part[2 * o] = mix(masks.m2, up<2>(h), l);
+                    part[2 * o + 1] = mix(masks.m2, h, down<2>(l));
+                } else {
+                    v4i out;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const int i = k * NT + nt, ahead = i + BR - 1;
-                    if (ahead < KS * NT) br[ahead % BR] = codes(ahead / NT, ahead % NT);
-#pragma unroll
-                    for (int d = 0; d < 4; ++d)
-                        acc[d][nt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, now[d]), br[i % BR], acc[d][nt], 0, 0, 0);
-                    __builtin_amdgcn_sched_barrier(0);
+                    for (int k = 0; k < 2; ++k) {
+                        const uint64_t x = part[k], y = Q == 2 ? part[2 + k] : 0;
+                        const uint64_t r = o ? mix(masks.m4, x, Q == 2 ? down<4>(y) : 0) : mix(masks.m4, up<4>(x), y);
+                        out[2 * k] = (int)(uint32_t)r;
+                        out[2 * k + 1] = (int)(r >> 32);
+                    }
+                    *reinterpret_cast<v4i *>(to + t * 512 + o * 256) = out;
                 }
-                if (KS == 1) {
+            };
+            v4i acc[ND][NT];
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) now[d] = next[d];
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) acc[d][nt] = v4i{0, 0, 0, 0};
+            u32x4 ar[AR][ND];
+            auto load_digits = [&](u32x4 (&dst)[ND], int step) {
+#pragma unroll
+                for (int d = 0; d < ND; ++d) dst[d] = __builtin_amdgcn_raw_buffer_load_b128(rd, lane * 16 + d * 1024, step * 4096, 0);
+            };
+            issue(w[0], 0);
+#pragma unroll
+            for (int i = 0; i < AR - 1; ++i) load_digits(ar[i], i);
+#pragma unroll
+            for (int i = 0; i < STAGES; ++i) expand(i, w[0], 0, my_codes);
+#pragma unroll
+            for (int i = 1; i <= WS; ++i) issue(w[i % WS], i);
+            __syncthreads();
+            for (int turn = 0; turn < loops; turn += UL) {
+#pragma unroll
+                for (int u = 0; u < UL; ++u) {
+                    const int loop = turn + u;
+                    if (loop < loops) {
+                        const int here = loop & 1 ? BUF : 0;
+                        const unsigned char *src = operands + here;
+                        unsigned char *const to = my_codes + (BUF - here);
+                        // operand nt of step k of the buffer
+                        auto codes = [&](int k, int nt) {
+                            const unsigned char *at = src + k * 4 * TILE + nt * 256;
+                            const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((v2i __attribute__((address_space(3))) *)(at));
+                            const v2i y = __builtin_amdgcn_ds_read_tr8_b64_v2i32((v2i __attribute__((address_space(3))) *)(at + 128));
+                            return v4i{x[0], x[1], y[0], y[1]};
+                        };
+                        v4i br[BR];
+#pragma unroll
+                        for (int i = 0; i < BR - 1; ++i) br[i] = codes(0, i);
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int k = 0; k < KS; ++k) {
+                            const int c = u * KS + k;
+                            load_digits(ar[(c + AR - 1) % AR], loop * KS + k + AR - 1);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                const int i = k * NT + nt, ahead = i + BR - 1;
+                                if (ahead < KS * NT) br[ahead % BR] = codes(ahead / NT, ahead % NT);
+                                // (the next buffer's codes)
+                                constexpr int AT_ONCE = KS * NT >= 48 ? 1 : (KS * NT >= 24 ? 2 : 3);
+#pragma unroll
+                                for (int x = AT_ONCE * i; x < AT_ONCE * i + AT_ONCE && x < STAGES; ++x) {
+                                    expand(x, w[(u + 1) % WS], loop + 1, to);
+                                    if (x == 19) issue(w[(u + 1) % WS], loop + 1 + WS);     // (the last word is on its way)
+                                }
+#pragma unroll
+                                for (int d = 0; d < ND; ++d)
+                                    acc[d][nt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, ar[c % AR][d]), br[i % BR], acc[d][nt], 0, 0, 0);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                        }
+                        __syncthreads();
+                    }
+                }
+            }
+            // ---- a lane has column j of every sixteen and the vectors 4 kb + c ----
+            int at = lane;
+            asm volatile("" : "+v"(at));       // (the addresses of the results are worked out here and not kept during the loop)
+            const int jj = at & 15, first = group * kGroupVectors + (at >> 4) * 4;
+            const int slot = e - 1 - l0;
+            const double s = (double)s_scales[e - 1], gscale = ldexp(slot == 0 ? -s : s, slot - 7);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int n = first + c;
+                if (n < a.batch) {
+                    const int ex = ND == 3 ? a.scalings[n].e3 : a.scalings[n].e4;
+                    const double factor = ex == kNotFinite ? (double)NAN : ldexp(gscale, -ex);
+                    float *out = a.out + ((size_t)split * a.batch + n) * a.cols;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const int g = wn * NT + nt, h = g & 1, word = part_of_chunk * (16 / S::PARTS) + (g >> 1);
+                        const int col = q * 512 + word * 32 + 8 * (jj & 3) + 4 * h + (jj >> 2);
+                        if (col < a.cols) {
+                            double v = fma(256.0, (double)acc[1][nt][c], (double)acc[0][nt][c]);
+                            v = fma(65536.0, (double)acc[2][nt][c], v);
+                            if constexpr (ND == 4) v = fma(16777216.0, (double)acc[3][nt][c], v);
+                            const float y = (float)(v * factor);
+                            out[col] = f == 0 ? y : out[col] + y;      // (later groups of bitlayers add to the thread's own result)
+                        }
+                    }
                 }
             }
             __syncthreads();
         }
-        // ---- a lane has column j of every sixteen and the vectors 4 kb + c ----
-        int jj = j;
-        asm volatile("" : "+v"(jj));       // (the addresses of the results are worked out here and not kept during the loop)
-        const int slot = e - 1 - l0;
-        const double s = (double)s_scales[e - 1], gscale = ldexp(slot == 0 ? -s : s, slot - 7);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const int n = group * kGroupVectors + kb * 4 + c;
-            if (n < a.batch) {
-                const int ex = a.exps[n];
-                const double factor = ex == kNotFinite ? (double)NAN : ldexp(gscale, -ex);
-                float *out = a.out + ((size_t)blockIdx.z * a.batch + n) * a.cols;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const int g = wn * NT + nt, h = g & 1, word = GROUPS == 32 ? g >> 1 : (g >> 2) * 4 + my_half * 2 + ((g >> 1) & 1);
-                    const int col = q * 512 + word * 32 + 8 * (jj & 3) + 4 * h + (jj >> 2);
-                    if (col < a.cols) {
-                        const double v = fma(16777216.0, (double)acc[3][nt][c],
-                                             fma(65536.0, (double)acc[2][nt][c], fma(256.0, (double)acc[1][nt][c], (double)acc[0][nt][c])));
-                        const float y = (float)(v * factor);
-                        out[col] = first ? y : out[col] + y;      // (later groups of bitlayers add to the thread's own result)
-                    }
-                }
-            }
+    };
+    // (the waves of a workgroup may differ: both ways pass the same barriers)
+    if constexpr (WM >= 4) {
+        const int n = group * kGroupVectors + j;
+        Scaling mine = {0, 0, 0, 0};
+        if (n < a.batch) mine = a.scalings[n];
+        if (a.may_narrow && !group_is_wide(mine, n < a.batch)) {
+            sum_up(std::integral_constant<int, 3>{}, std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
+            return;
         }
-        first = false;
-        __syncthreads();
+        sum_up(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{}, std::integral_constant<int, 1>{});
+    } else {
+        sum_up(std::integral_constant<int, 4>{}, std::integral_constant<int, WM == 1 ? 4 : 2>{}, std::integral_constant<int, WM == 1 ? 2 : 1>{});
     }
 }
 
@@ -301,17 +437,18 @@ __global__ __launch_bounds__(256) void k_grad_join(const float *__restrict__ par
 
 // ---------------------------------------------------------------------------------------------------------------
 
-// How a call is shared out; the workspace holds [exponents][digits][parts of the split sum]
+// How a call is shared out; the workspace holds [scalings][digits][parts of the split sum]
 struct GradPlan {
-    int wm, blocks, steps, splits, steps_per_split;
+    int wm, blocks, ks, steps, splits, steps_per_split;
     size_t digits_off, parts_off, bytes;
 };
 constexpr int kGradCus = 256;
 static GradPlan grad_plan(const Layout &L, int batch)
 {
     GradPlan p;
-    p.wm = batch <= 16 ? 1 : (batch <= 32 ? 2 : 4);
-    p.blocks = L.cq * (p.wm == 4 ? 2 : 1);
+    p.wm = batch <= 16 ? 1 : (batch <= 32 ? 2 : (batch <= 64 ? 4 : 8));
+    p.blocks = L.cq * (p.wm == 8 ? 4 : (p.wm == 4 ? 2 : 1));
+    p.ks = p.wm == 8 ? 8 : (p.wm == 4 ? 4 : 2);
     p.steps = (L.rt_count + 3) / 4;
     const int rows_of = (batch + 16 * p.wm - 1) / (16 * p.wm);
     int splits = kGradCus / (p.blocks * rows_of);
@@ -319,41 +456,43 @@ static GradPlan grad_plan(const Layout &L, int batch)
     if (splits < 1) splits = 1;
     const int least = (p.steps + 1023) / 1024;        // (int32 sums: 65536 rows)
     if (splits < least) splits = least;
-    p.steps_per_split = ((p.steps + splits - 1) / splits + 1) & ~1;      // (whole buffers)
+    p.steps_per_split = ((p.steps + splits - 1) / splits + p.ks - 1) / p.ks * p.ks;      // (whole buffers)
     p.splits = (p.steps + p.steps_per_split - 1) / p.steps_per_split;
     auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
-    p.digits_off = up((size_t)batch * 4);
+    p.digits_off = up((size_t)batch * sizeof(Scaling));
     p.parts_off = p.digits_off + (size_t)((batch + 15) / 16) * (size_t)p.steps * 4096;
     p.bytes = p.parts_off + (p.splits > 1 ? up((size_t)p.splits * batch * L.cols * 4) : 0);
     return p;
 }
 size_t grad_workspace_bytes(const Layout &L, int batch) { return grad_plan(L, batch).bytes; }
 
-template <int WM>
-static const void *grad_kernel(bool wide, bool il)
-{
-    if (wide) return il ? reinterpret_cast<const void *>(k_grad<2, true, WM>) : reinterpret_cast<const void *>(k_grad<2, false, WM>);
-    return il ? reinterpret_cast<const void *>(k_grad<1, true, WM>) : reinterpret_cast<const void *>(k_grad<1, false, WM>);
-}
+#define PB_GRAD(WM) {{reinterpret_cast<const void *>(k_grad<1, false, WM>), reinterpret_cast<const void *>(k_grad<1, true, WM>)}, \
+                     {reinterpret_cast<const void *>(k_grad<2, false, WM>), reinterpret_cast<const void *>(k_grad<2, true, WM>)}}
+static const void *const kGradFn[4][2][2] = {PB_GRAD(1), PB_GRAD(2), PB_GRAD(4), PB_GRAD(8)};
+constexpr int kGradLds[4] = {GradShape<1>::LDS, GradShape<2>::LDS, GradShape<4>::LDS, GradShape<8>::LDS};
 
 int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, int bits_used, const float *dY, const GatedSource *gated,
                 int batch, float *dX, void *workspace, hipStream_t st)
 {
     const GradPlan p = grad_plan(L, batch);
     char *const ws = static_cast<char *>(workspace);
-    int *const exps = reinterpret_cast<int *>(ws);
+    Scaling *const scalings = reinterpret_cast<Scaling *>(ws);
     uint8_t *const digits = reinterpret_cast<uint8_t *>(ws + p.digits_off);
     if (gated) {
         hipLaunchKernelGGL(k_gated_grad, dim3((unsigned)batch), dim3(1024), 0, st, gated->pre, gated->dH, L.rows / 2, gated->gate, gated->dpre,
-                           exps);
+                           scalings);
         dY = gated->dpre;
     } else {
-        hipLaunchKernelGGL(k_grad_exponents, dim3((unsigned)batch), dim3(1024), 0, st, dY, L.rows, exps);
+        hipLaunchKernelGGL(k_grad_scalings, dim3((unsigned)batch), dim3(1024), 0, st, dY, L.rows, scalings);
     }
     int err = (int)hipGetLastError();
     if (err) return err;
-    hipLaunchKernelGGL(k_grad_digits, dim3((unsigned)((p.steps + 3) / 4), (unsigned)((batch + 15) / 16)), dim3(256), 0, st, dY, exps, batch,
-                       L.rows, L.gate_h, p.steps, digits);
+    const dim3 by_steps((unsigned)((p.steps + 3) / 4), (unsigned)((batch + 15) / 16));
+    const int may_narrow = p.wm >= 4;
+    if ((L.gate_h ? L.gate_h : L.rows) % 4 == 0)
+        hipLaunchKernelGGL(k_grad_digits<true>, by_steps, dim3(256), 0, st, dY, scalings, batch, L.rows, L.gate_h, p.steps, may_narrow, digits);
+    else
+        hipLaunchKernelGGL(k_grad_digits<false>, by_steps, dim3(256), 0, st, dY, scalings, batch, L.rows, L.gate_h, p.steps, may_narrow, digits);
     err = (int)hipGetLastError();
     if (err) return err;
     GradArgs a;
@@ -363,14 +502,22 @@ int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, in
     a.round_step = (uint32_t)(tile16_rowtile_stride(L) * 4);
     a.rt_count = L.rt_count; a.cq = L.cq; a.m = bits_used; a.batch = batch; a.cols = L.cols;
     a.steps = p.steps; a.steps_per_split = p.steps_per_split;
-    a.scales = scales; a.digits = digits; a.exps = exps;
+    a.scales = scales; a.digits = digits; a.scalings = scalings; a.may_narrow = may_narrow;
+    a.blocks = p.blocks; a.rows_of = (batch + 16 * p.wm - 1) / (16 * p.wm);
+    a.workgroups = a.blocks * a.rows_of * p.splits;
     float *const parts = reinterpret_cast<float *>(ws + p.parts_off);
     a.out = p.splits > 1 ? parts : dX;
-    const bool wide = bits_used > 4, il = is_pairs(L.layout);
-    const void *fn = p.wm == 1 ? grad_kernel<1>(wide, il) : (p.wm == 2 ? grad_kernel<2>(wide, il) : grad_kernel<4>(wide, il));
+    const int shape = p.wm == 8 ? 3 : p.wm / 2, wide = bits_used > 4, il = is_pairs(L.layout);
+    const void *fn = kGradFn[shape][wide][il];
+    static bool declared[4][2][2];      // (more than the default 64 KB of LDS)
+    hipError_t e = hipSuccess;
+    if (!__atomic_load_n(&declared[shape][wide][il], __ATOMIC_RELAXED)) {
+        e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kGradLds[shape]);
+        if (e != hipSuccess) return (int)e;
+        __atomic_store_n(&declared[shape][wide][il], true, __ATOMIC_RELAXED);
+    }
     void *args[] = {&a};
-    const dim3 grid((unsigned)p.blocks, (unsigned)((batch + 16 * p.wm - 1) / (16 * p.wm)), (unsigned)p.splits);
-    hipError_t e = hipLaunchKernel(fn, grid, dim3(512), args, 0, st);
+    e = hipLaunchKernel(fn, dim3((unsigned)a.workgroups), dim3(512), args, (size_t)kGradLds[shape], st);
     if (e == hipSuccess) e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
     if (p.splits > 1) {

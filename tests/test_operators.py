@@ -160,8 +160,10 @@ def close(got, want, tol, what):
 
 
 def grad_tolerance(dY, W, parts):
-    """dY rounded to 2^-30 of its vector's largest value at most; `parts` sums rounded to fp32 and added one after the other."""
-    return 2.0 ** -30 * np.abs(dY).max(axis=1, keepdims=True) * np.abs(W).sum(axis=0) + 2 * parts * U * (np.abs(dY) @ np.abs(W))
+    """dY rounded to 2^-30 of its vector's largest value at most (four digits), or to half a unit of three digits, the largest value being 2^22 to
+    2^23 units, 0.998 * 2^22 where the scaling is one less; `parts` sums rounded to fp32 and added one after the other."""
+    half_a_unit = 2.0 ** -30 if len(dY) <= 32 else 2.0 ** -23 / 0.998
+    return half_a_unit * np.abs(dY).max(axis=1, keepdims=True) * np.abs(W).sum(axis=0) + 2 * parts * U * (np.abs(dY) @ np.abs(W))
 
 
 LAYOUTS = {"bits": 0x50420002, "gates": 0x50420003, "pairs": 0x50420004, "rows": 0x50420001}
