@@ -68,10 +68,18 @@ __global__ __launch_bounds__(1024) void k_grad_scalings(const float *__restrict_
     const float *y = dY + (size_t)blockIdx.x * rows;
     uint32_t most = 0;
     double squares = 0.0;
-    for (int r = threadIdx.x; r < rows; r += 1024) {
-        const float v = y[r];
+    auto take = [&](float v) {
         most = max(most, __float_as_uint(v) & 0x7FFFFFFFu);
         squares = fma((double)v, (double)v, squares);
+    };
+    if (rows % 4 == 0) {
+#pragma unroll 4
+        for (int r = threadIdx.x * 4; r < rows; r += 4096) {
+            const float4 v = *reinterpret_cast<const float4 *>(y + r);
+            take(v.x); take(v.y); take(v.z); take(v.w);
+        }
+    } else {
+        for (int r = threadIdx.x; r < rows; r += 1024) take(y[r]);
     }
     over_workgroup<16>(most, squares);
     if (threadIdx.x == 0) scalings[blockIdx.x] = scaling_of(most, squares, rows);
@@ -86,14 +94,28 @@ __global__ __launch_bounds__(1024) void k_gated_grad(const float *__restrict__ p
     float *dg = dpre + n * 2 * units, *du = dg + units;
     uint32_t most = 0;
     double squares = 0.0;
-    for (int r = threadIdx.x; r < units; r += 1024) {
+    auto one = [&](float g, float u, float dh, float *dg, float *du) {
         float a, da;
-        gate_with_slope(gate, g[r], &a, &da);
-        const float x = dh[r] * u[r] * da, y = dh[r] * a;
-        dg[r] = x;
-        du[r] = y;
+        gate_with_slope(gate, g, &a, &da);
+        const float x = dh * u * da, y = dh * a;
+        *dg = x;
+        *du = y;
         most = max(most, max(__float_as_uint(x) & 0x7FFFFFFFu, __float_as_uint(y) & 0x7FFFFFFFu));
         squares = fma((double)x, (double)x, fma((double)y, (double)y, squares));
+    };
+    if (units % 2 == 0) {       // (a vector of 2 units values begins at a multiple of 16 bytes, its second half at one of 8)
+#pragma unroll 2
+        for (int r = threadIdx.x * 2; r < units; r += 2048) {
+            const float2 vg = *reinterpret_cast<const float2 *>(g + r), vu = *reinterpret_cast<const float2 *>(u + r);
+            const float2 vh = *reinterpret_cast<const float2 *>(dh + r);
+            float2 x, y;
+            one(vg.x, vu.x, vh.x, &x.x, &y.x);
+            one(vg.y, vu.y, vh.y, &x.y, &y.y);
+            *reinterpret_cast<float2 *>(dg + r) = x;
+            *reinterpret_cast<float2 *>(du + r) = y;
+        }
+    } else {
+        for (int r = threadIdx.x; r < units; r += 1024) one(g[r], u[r], dh[r], dg + r, du + r);
     }
     over_workgroup<16>(most, squares);
     if (threadIdx.x == 0) scalings[n] = scaling_of(most, squares, 2 * units);
@@ -220,7 +242,6 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
     const int step0 = split * a.steps_per_split, step1 = min(step0 + a.steps_per_split, a.steps);   // (not empty)
     const int loops = (step1 - step0 + KS - 1) / KS;
     const int m = a.m;
-    const Masks masks = make_masks();
 
     // the scales: whether they halve (as in k_i8_tile)
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.scales), 0, m * 4, 0x00020000);
@@ -243,12 +264,13 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
     // where the wave's operands begin in a buffer
     const unsigned char *const operands = s_codes + kb * TILE + wn * NT * 256 + j * 8;
 
-    // Everything of the sum over the rows with ND digits: AR sets of registers for the digits of as many steps, WS for the words of as many buffers
-    auto sum_up = [&](auto nd, auto ar_sets, auto word_sets) {
-        constexpr int ND = decltype(nd)::value, AR = decltype(ar_sets)::value, WS = decltype(word_sets)::value;
-        constexpr int UL = AR > KS ? AR / KS : 1;           // buffers until the sets of registers are the first ones again
-        constexpr int BR = WM >= 4 && ND == 4 ? 2 : 3;      // operands of codes on their way from LDS (the registers are full with four digits)
-        static_assert(UL * KS % AR == 0 && (WS == 1 || UL % WS == 0), "whole turns");
+    // everything of the sum over the rows with ND digits
+    auto sum_up = [&](auto nd) {
+        constexpr int ND = decltype(nd)::value;
+        // digits at once: where the sums of four digits nearly fill the registers, the codes are read twice, for two digits each
+        constexpr int DC = WM >= 4 && ND == 4 ? 2 : ND, TURNS = KS * (ND / DC);
+        constexpr int BR = 3;                               // operands of codes on their way from LDS
+        static_assert(TURNS % 2 == 0, "the digits of two turns share the registers");
         for (int f = 0, e; f < m; f = e) {
             e = min(m, f + (f == 0 ? gs0 : gs1));
             const int l0 = (f & ~1) == 0 ? 0 : (f & ~1) - 2;
@@ -259,11 +281,12 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
                 mask[p] = (l >= f && l < e ? 0xAAAAAAAAu : 0u) | (l + 1 >= f && l + 1 < e ? 0x55555555u : 0u);
             }
             const uint32_t flip = l0 == 0 ? 0xAAAAAAAAu : 0u;
-            u32x4 w[WS][4 * Q];
+            const Masks masks = make_masks();
+            u32x4 w[4 * Q];
             // the words of buffer `loop`; those of row tiles beyond the end are zero
             const int end = min(a.rt_count, step1 * 4);
             auto inside = [&](int loop) { return (step0 + loop * KS) * 4 + my_tile < end; };
-            auto issue = [&](u32x4 (&w)[4 * Q], int loop) {
+            auto issue = [&](int loop) {
                 const uint32_t at = (uint32_t)((step0 + loop * KS) * 4 + wave * (TILES / 8)) * a.round_step + (uint32_t)q * 1024u;
                 const int mine = inside(loop) ? (int)my_at : -16;      // (beyond every buffer)
 #pragma unroll
@@ -280,7 +303,7 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
             constexpr int STAGES = 24;
             uint64_t part[4];         // first h, l (then the nibbles' two halves), second h, l
             uint32_t keep[2 * Q];     // (IL)
-            auto expand = [&](int stage, const u32x4 (&w)[4 * Q], int loop, unsigned char *to) {
+            auto expand = [&](int stage, int loop, unsigned char *to) {
                 const int t = stage / 6, o = stage & 1;
                 if (stage % 6 < 2) {
                     if (stage == 0) {
@@ -318,67 +341,64 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
                     *reinterpret_cast<v4i *>(to + t * 512 + o * 256) = out;
                 }
             };
+            u32x4 ar[2][DC];
+            auto load_digits = [&](u32x4 (&dst)[DC], int step, int from) {
+#pragma unroll
+                for (int d = 0; d < DC; ++d) dst[d] = __builtin_amdgcn_raw_buffer_load_b128(rd, lane * 16, step * 4096 + (from + d) * 1024, 0);
+            };
+            issue(0);
+            load_digits(ar[0], 0, 0);
+#pragma unroll
+            for (int i = 0; i < STAGES; ++i) {
+                expand(i, 0, my_codes);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            issue(1);
+            __syncthreads();
             v4i acc[ND][NT];
 #pragma unroll
             for (int d = 0; d < ND; ++d)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) acc[d][nt] = v4i{0, 0, 0, 0};
-            u32x4 ar[AR][ND];
-            auto load_digits = [&](u32x4 (&dst)[ND], int step) {
+            for (int loop = 0; loop < loops; ++loop) {
+                const int here = loop & 1 ? BUF : 0;
+                const unsigned char *src = operands + here;
+                unsigned char *const to = my_codes + (BUF - here);
+                // operand nt of step k of the buffer
+                auto codes = [&](int k, int nt) {
+                    const unsigned char *at = src + k * 4 * TILE + nt * 256;
+                    const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((v2i __attribute__((address_space(3))) *)(at));
+                    const v2i y = __builtin_amdgcn_ds_read_tr8_b64_v2i32((v2i __attribute__((address_space(3))) *)(at + 128));
+                    return v4i{x[0], x[1], y[0], y[1]};
+                };
+                v4i br[BR];
 #pragma unroll
-                for (int d = 0; d < ND; ++d) dst[d] = __builtin_amdgcn_raw_buffer_load_b128(rd, lane * 16 + d * 1024, step * 4096, 0);
-            };
-            issue(w[0], 0);
+                for (int i = 0; i < BR - 1; ++i) br[i] = codes(0, i);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < AR - 1; ++i) load_digits(ar[i], i);
+                for (int k = 0; k < TURNS; ++k) {
+                    // (turn k: step k / (TURNS / KS) of the buffer, the digits from k % (TURNS / KS) * DC on)
+                    load_digits(ar[(k + 1) & 1], loop * KS + (k + 1) / (TURNS / KS), (k + 1) % (TURNS / KS) * DC);
 #pragma unroll
-            for (int i = 0; i < STAGES; ++i) expand(i, w[0], 0, my_codes);
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const int i = k * NT + nt, ahead = i + BR - 1;
+                        if (ahead < TURNS * NT) br[ahead % BR] = codes(ahead / NT / (TURNS / KS), ahead % NT);
+                        // (the next buffer's codes, in the first half of the loop: the words after them then have the second half to arrive)
+                        constexpr int AT_ONCE = 48 / (TURNS * NT) > 1 ? 48 / (TURNS * NT) : 1;
 #pragma unroll
-            for (int i = 1; i <= WS; ++i) issue(w[i % WS], i);
-            __syncthreads();
-            for (int turn = 0; turn < loops; turn += UL) {
-#pragma unroll
-                for (int u = 0; u < UL; ++u) {
-                    const int loop = turn + u;
-                    if (loop < loops) {
-                        const int here = loop & 1 ? BUF : 0;
-                        const unsigned char *src = operands + here;
-                        unsigned char *const to = my_codes + (BUF - here);
-                        // operand nt of step k of the buffer
-                        auto codes = [&](int k, int nt) {
-                            const unsigned char *at = src + k * 4 * TILE + nt * 256;
-                            const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((v2i __attribute__((address_space(3))) *)(at));
-                            const v2i y = __builtin_amdgcn_ds_read_tr8_b64_v2i32((v2i __attribute__((address_space(3))) *)(at + 128));
-                            return v4i{x[0], x[1], y[0], y[1]};
-                        };
-                        v4i br[BR];
-#pragma unroll
-                        for (int i = 0; i < BR - 1; ++i) br[i] = codes(0, i);
-                        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                        for (int k = 0; k < KS; ++k) {
-                            const int c = u * KS + k;
-                            load_digits(ar[(c + AR - 1) % AR], loop * KS + k + AR - 1);
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                const int i = k * NT + nt, ahead = i + BR - 1;
-                                if (ahead < KS * NT) br[ahead % BR] = codes(ahead / NT, ahead % NT);
-                                // (the next buffer's codes)
-                                constexpr int AT_ONCE = KS * NT >= 48 ? 1 : (KS * NT >= 24 ? 2 : 3);
-#pragma unroll
-                                for (int x = AT_ONCE * i; x < AT_ONCE * i + AT_ONCE && x < STAGES; ++x) {
-                                    expand(x, w[(u + 1) % WS], loop + 1, to);
-                                    if (x == 19) issue(w[(u + 1) % WS], loop + 1 + WS);     // (the last word is on its way)
-                                }
-#pragma unroll
-                                for (int d = 0; d < ND; ++d)
-                                    acc[d][nt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, ar[c % AR][d]), br[i % BR], acc[d][nt], 0, 0, 0);
-                                __builtin_amdgcn_sched_barrier(0);
-                            }
+                        for (int x = AT_ONCE * i; x < AT_ONCE * i + AT_ONCE && x < STAGES; ++x) {
+                            expand(x, loop + 1, to);
+                            if (x == 19) issue(loop + 2);       // (the last word has been taken)
                         }
-                        __syncthreads();
+#pragma unroll
+                        for (int d = 0; d < DC; ++d) {
+                            v4i &sum = acc[k % (TURNS / KS) * DC + d][nt];
+                            sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, ar[k & 1][d]), br[i % BR], sum, 0, 0, 0);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
                     }
                 }
+                __syncthreads();
             }
             // ---- a lane has column j of every sixteen and the vectors 4 kb + c ----
             int at = lane;
@@ -416,23 +436,37 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
         Scaling mine = {0, 0, 0, 0};
         if (n < a.batch) mine = a.scalings[n];
         if (a.may_narrow && !group_is_wide(mine, n < a.batch)) {
-            sum_up(std::integral_constant<int, 3>{}, std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
+            sum_up(std::integral_constant<int, 3>{});
             return;
         }
-        sum_up(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{}, std::integral_constant<int, 1>{});
+        sum_up(std::integral_constant<int, 4>{});
     } else {
-        sum_up(std::integral_constant<int, 4>{}, std::integral_constant<int, WM == 1 ? 4 : 2>{}, std::integral_constant<int, WM == 1 ? 2 : 1>{});
+        sum_up(std::integral_constant<int, 4>{});
     }
 }
 
 // The parts of a split sum, in the order of the rows
 __global__ __launch_bounds__(256) void k_grad_join(const float *__restrict__ parts, int splits, size_t total, float *__restrict__ dX)
 {
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 2;
     if (i >= total) return;
-    float v = parts[i];
-    for (int s = 1; s < splits; ++s) v += parts[(size_t)s * total + i];
-    dX[i] = v;
+    if (total % 2 == 0) {
+        float2 v = *reinterpret_cast<const float2 *>(parts + i);
+#pragma unroll 8
+        for (int s = 1; s < splits; ++s) {
+            const float2 w = *reinterpret_cast<const float2 *>(parts + (size_t)s * total + i);
+            v.x += w.x;
+            v.y += w.y;
+        }
+        *reinterpret_cast<float2 *>(dX + i) = v;
+    } else {
+        for (size_t k = i; k < i + 2 && k < total; ++k) {
+            float v = parts[k];
+#pragma unroll 8
+            for (int s = 1; s < splits; ++s) v += parts[(size_t)s * total + k];
+            dX[k] = v;
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -451,13 +485,18 @@ static GradPlan grad_plan(const Layout &L, int batch)
     p.ks = p.wm == 8 ? 8 : (p.wm == 4 ? 4 : 2);
     p.steps = (L.rt_count + 3) / 4;
     const int rows_of = (batch + 16 * p.wm - 1) / (16 * p.wm);
-    int splits = kGradCus / (p.blocks * rows_of);
-    if (splits > p.steps / 4) splits = p.steps / 4;
-    if (splits < 1) splits = 1;
-    const int least = (p.steps + 1023) / 1024;        // (int32 sums: 65536 rows)
-    if (splits < least) splits = least;
-    p.steps_per_split = ((p.steps + splits - 1) / splits + p.ks - 1) / p.ks * p.ks;      // (whole buffers)
-    p.splits = (p.steps + p.steps_per_split - 1) / p.steps_per_split;
+    // Parts of the sum: rounds of workgroups over the chip (one per compute unit), each of so many us for its start and end and for a step; more
+    // than one part costs the way of the parts through memory and a launch.
+    const double step = p.wm == 8 ? 0.67 : (p.wm == 4 ? 0.75 : 1.5);
+    double least_time = 1e30;
+    p.splits = 1;
+    for (int splits = (p.steps + 1023) / 1024, n = 0; n < 64; ++splits, ++n) {       // (int32 sums: 65536 rows)
+        const int each = ((p.steps + splits - 1) / splits + p.ks - 1) / p.ks * p.ks, parts = (p.steps + each - 1) / each;   // (whole buffers)
+        if (parts < splits && n) continue;
+        const double rounds = (double)(((long long)p.blocks * rows_of * parts + kGradCus - 1) / kGradCus);
+        const double time = rounds * (3.0 + step * each) + (parts > 1 ? 3.0 + (parts + 2) * 4e-6 * batch * L.cols / 4.0 : 0.0);
+        if (time < least_time) { least_time = time; p.splits = parts; p.steps_per_split = each; }
+    }
     auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
     p.digits_off = up((size_t)batch * sizeof(Scaling));
     p.parts_off = p.digits_off + (size_t)((batch + 15) / 16) * (size_t)p.steps * 4096;
@@ -522,7 +561,7 @@ int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, in
     if (e != hipSuccess) return (int)e;
     if (p.splits > 1) {
         const size_t total = (size_t)batch * L.cols;
-        hipLaunchKernelGGL(k_grad_join, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, parts, p.splits, total, dX);
+        hipLaunchKernelGGL(k_grad_join, dim3((unsigned)((total + 511) / 512)), dim3(256), 0, st, parts, p.splits, total, dX);
         e = hipGetLastError();
     }
     return (int)e;
