@@ -65,31 +65,85 @@ __device__ __forceinline__ v4f mfma(float a, float b, v4f c) { return __builtin_
 // ---- the order of the vectors ----
 struct Item { int adapter, start, length, pad; };     // places start .. start + length of the order
 
+// The r-th of the lanes that are set in `mask`, in lane r
+__device__ __forceinline__ int lanes_in_order(unsigned long long mask, int lane)
+{
+    const bool set = mask >> lane & 1;
+    const int rank = __popcll(mask & ((1ull << lane) - 1));
+    // (the lanes that are not set go behind the others)
+    return __builtin_amdgcn_ds_permute((set ? rank : __popcll(mask) + lane - rank) * 4, lane);
+}
+// The lanes with the same key as this one, of those with a key of 0 or more
+__device__ __forceinline__ unsigned long long same_key(int key, int count)
+{
+    unsigned long long mask = __builtin_amdgcn_ballot_w64(key >= 0);
+    for (int b = 0; (count - 1) >> b; ++b) {
+        const unsigned long long set = __builtin_amdgcn_ballot_w64((key >> b & 1) != 0);
+        mask &= (key >> b & 1) ? set : ~set;
+    }
+    return mask;
+}
+
 // What the kernels go by: the order of the vectors, its tiles, and where an adapter's vectors begin in it.  Without an index all vectors have
-// adapter 0 and their own order, and none of the arrays is there.
+// adapter 0 and their own order.  Up to 64 vectors every wave works the order out from the index; for more k_adapter_order has left it in memory.
 struct Order {
+    const int32_t *index;
     const int *order;
     const Item *items;
     const int *counts;        // [0]: tiles
     const int *starts;        // [adapter], and the end
-    int batch;
-    __device__ bool tile(int i, Item *t) const
+    int batch, count;
+
+    __device__ int key_of(int n) const
     {
-        if (!order) {
-            *t = {0, i * 16, min(16, batch - i * 16), 0};
+        const int k = n < batch ? index[n] : -1;
+        return k >= 0 && k < count ? k : -1;
+    }
+    // Tile i: its adapter, its vectors, and vector lane % 16 of them (of a lane beyond: any of the tile)
+    struct Tile { int adapter, length, vector; };
+    __device__ bool tile(int i, int lane, Tile *t) const
+    {
+        if (!index) {
+            *t = {0, min(16, batch - i * 16), min(i * 16 + (lane & 15), batch - 1)};
             return i * 16 < batch;
         }
-        if (i >= counts[0]) return false;
-        *t = items[i];
+        if (order) {
+            if (i >= counts[0]) return false;
+            const Item it = items[i];
+            *t = {it.adapter, it.length, order[it.start + min(lane & 15, it.length - 1)]};
+            return true;
+        }
+        const int key = key_of(lane);
+        const unsigned long long same = same_key(key, count), below = (1ull << lane) - 1;
+        const int place = __popcll(same & below);
+        const bool begins = key >= 0 && place % 16 == 0;
+        const unsigned long long all = __builtin_amdgcn_ballot_w64(begins);
+        if (i >= __popcll(all)) return false;
+        const int first = __builtin_ctzll(__builtin_amdgcn_ballot_w64(begins && __popcll(all & below) == i));
+        const unsigned long long mine =
+            (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(same >> 32), first) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)same, first);
+        t->adapter = __builtin_amdgcn_readlane(key, first);
+        const unsigned long long left = mine >> first << first;      // (it and those behind it)
+        t->length = min(16, __popcll(left));
+        t->vector = __shfl(lanes_in_order(left, lane), min(lane & 15, t->length - 1));
         return true;
     }
-    __device__ int vector(int place) const { return order ? order[place] : place; }
-    __device__ void segment(int adapter, int *start, int *end) const
+    // The vectors of an adapter: `length` of them, number p is vector(p)
+    struct Segment {
+        const int *order;
+        int length, list;     // list: lane r has number r, if `listed`
+        bool listed;
+        __device__ int vector(int p) const { return listed ? __shfl(list, p) : (order ? order[p] : p); }
+    };
+    __device__ Segment segment(int adapter, int lane) const
     {
-        *start = order ? starts[adapter] : (adapter ? batch : 0);
-        *end = order ? starts[adapter + 1] : batch;
+        if (!index) return {nullptr, adapter ? 0 : batch, 0, false};
+        if (order) return {order + starts[adapter], starts[adapter + 1] - starts[adapter], 0, false};
+        const unsigned long long mine = __builtin_amdgcn_ballot_w64(key_of(lane) == adapter);
+        return {nullptr, (int)__popcll(mine), lanes_in_order(mine, lane), true};
     }
 };
+constexpr int kListed = 64;       // vectors of which no order is left in memory
 
 // One workgroup.  A wave finds out for 64 vectors which of them have the same adapter (a ballot per bit of its number), then the waves add to the
 // adapters' counts in the order of the vectors: the order within an adapter is theirs, so that sums over its vectors are the same every time.
@@ -108,16 +162,11 @@ __global__ __launch_bounds__(kOrderThreads) void k_adapter_order(const int32_t *
         const int n = (i * (kOrderThreads / 64) + wave) * 64 + lane;
         int k = n < batch ? index[n] : -1;
         if (k < 0 || k >= count) k = -1;
-        unsigned long long mask = __builtin_amdgcn_ballot_w64(k >= 0);
-        for (int b = 0; b < 12; ++b) {
-            const unsigned long long set = __builtin_amdgcn_ballot_w64((k >> b & 1) != 0);
-            mask &= (k >> b & 1) ? set : ~set;
-        }
+        const unsigned long long mask = same_key(k, count);
         key[i] = k;
         place[i] = __popcll(mask & ((1ull << lane) - 1));
         same[i] = __popcll(mask);
     }
-    static_assert(PB_MAX_ADAPTERS == 1 << 12, "twelve bits");
     const int chunks = (batch + 63) / 64;
 #pragma unroll
     for (int i = 0; i < kChunksPerWave; ++i)
@@ -172,45 +221,53 @@ struct DownArgs {
     const void *M;            // A or B
     const float *scale;       // (t only)
     const float *V;           // [batch][length]
-    float *out;               // [slice][place][16 ranks]: rank tile after rank tile, 16 values each
+    float *out;               // [slice][vector][16 ranks]: rank tile after rank tile, 16 values each
     int length, rank, ranks, slices;
 };
 // Parts of the sum of a tile's products go to the waves of `slices` workgroups; a lane's result is four ranks of one vector.
 //   TURNED: the summands are the rows of the matrix (B: [length][rank]), else its columns (A: [rank][length])
+constexpr int kDownWaves = 8;
 template <typename T, bool TURNED, bool VEC, int RT>
-__global__ __launch_bounds__(256) void k_adapter_down(const DownArgs a)
+__global__ __launch_bounds__(kDownWaves * 64) void k_adapter_down(const DownArgs a)
 {
-    __shared__ v4f s_part[3][RT][64];
+    __shared__ v4f s_part[kDownWaves - 1][RT][64];
     const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
-    Item it;
-    if (!a.order.tile(blockIdx.x, &it)) return;
+    Order::Tile it;
+    if (!a.order.tile(blockIdx.x, lane, &it)) return;
     const T *const M = static_cast<const T *>(a.M) + (size_t)it.adapter * a.rank * a.length;
-    const float *const x = a.V + (size_t)a.order.vector(it.start + min(i, it.length - 1)) * a.length;
+    const float *const x = a.V + (size_t)it.vector * a.length;
     const int rt0 = blockIdx.z * RT;
     v4f acc[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[t] = v4f{0, 0, 0, 0};
-    for (int c0 = (blockIdx.y * 4 + wave) * 64; c0 < a.length; c0 += a.slices * 256) {
+#pragma unroll 2
+    for (int c0 = (blockIdx.y * kDownWaves + wave) * 64; c0 < a.length; c0 += a.slices * kDownWaves * 64) {
+        v4f v[4], w[4][RT];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = load4_of<VEC>(x, c0 + 16 * q + 4 * kb, a.length);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int c = c0 + 16 * q + 4 * kb;
-            const v4f v = load4_of<VEC>(x, c, a.length);
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
                 const int j = (rt0 + t) * 16 + i;
-                v4f w = v4f{0, 0, 0, 0};
+                w[q][t] = v4f{0, 0, 0, 0};
                 if (j < a.rank) {
                     if constexpr (TURNED) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) w[e] = c + e < a.length ? to_f32(M[(size_t)(c + e) * a.rank + j]) : 0.0f;
+                        for (int e = 0; e < 4; ++e) w[q][t][e] = c + e < a.length ? to_f32(M[(size_t)(c + e) * a.rank + j]) : 0.0f;
                     } else {
-                        w = load4_of<VEC>(M + (size_t)j * a.length, c, a.length);
+                        w[q][t] = load4_of<VEC>(M + (size_t)j * a.length, c, a.length);
                     }
                 }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[t] = mfma(w[e], v[e], acc[t]);
             }
         }
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[t] = mfma(w[q][t][e], v[q][e], acc[t]);
     }
     if (wave > 0) {
 #pragma unroll
@@ -223,26 +280,27 @@ __global__ __launch_bounds__(256) void k_adapter_down(const DownArgs a)
     for (int t = 0; t < RT; ++t) {
         if (rt0 + t >= a.ranks) break;
         v4f v = acc[t];
-        for (int w = 0; w < 3; ++w) v += s_part[w][t][lane];
+#pragma unroll
+        for (int w = 0; w < kDownWaves - 1; ++w) v += s_part[w][t][lane];
         v *= s;
         // (ranks beyond the last are zero whatever the vector holds: 0 times infinity must not reach the products that follow)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if ((rt0 + t) * 16 + 4 * kb + e >= a.rank) v[e] = 0.0f;
-        *reinterpret_cast<v4f *>(a.out + (((size_t)blockIdx.y * a.order.batch + it.start + i) * a.ranks + rt0 + t) * 16 + 4 * kb) = v;
+        *reinterpret_cast<v4f *>(a.out + (((size_t)blockIdx.y * a.order.batch + it.vector) * a.ranks + rt0 + t) * 16 + 4 * kb) = v;
     }
 }
-// Ranks 4 part .. 4 part + 3 of rank tile `rt` at `place`: the slices added up in their order
-__device__ __forceinline__ v4f down_at(const float *parts, int slices, int batch, int ranks, int place, int rt, int part)
+// Ranks 4 part .. 4 part + 3 of rank tile `rt` of a vector: the slices added up in their order
+__device__ __forceinline__ v4f down_at(const float *parts, int slices, int batch, int ranks, int vector, int rt, int part)
 {
-    const float *p = parts + ((size_t)place * ranks + rt) * 16 + 4 * part;
+    const float *p = parts + ((size_t)vector * ranks + rt) * 16 + 4 * part;
     v4f v = *reinterpret_cast<const v4f *>(p);
     for (int s = 1; s < slices; ++s) v += *reinterpret_cast<const v4f *>(p + (size_t)s * batch * ranks * 16);
     return v;
 }
-__device__ __forceinline__ float down1_at(const float *parts, int slices, int batch, int ranks, int place, int rt, int i)
+__device__ __forceinline__ float down1_at(const float *parts, int slices, int batch, int ranks, int vector, int rt, int i)
 {
-    const float *p = parts + ((size_t)place * ranks + rt) * 16 + i;
+    const float *p = parts + ((size_t)vector * ranks + rt) * 16 + i;
     float v = *p;
     for (int s = 1; s < slices; ++s) v += p[(size_t)s * batch * ranks * 16];
     return v;
@@ -263,28 +321,33 @@ __global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
 {
     const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
     const int r0 = (blockIdx.x * 4 + wave) * 64;
-    Item it;
-    if (r0 >= a.length || !a.order.tile(blockIdx.y, &it)) return;
+    Order::Tile it;
+    if (r0 >= a.length || !a.order.tile(blockIdx.y, lane, &it)) return;
     const T *const M = static_cast<const T *>(a.M) + (size_t)it.adapter * a.rank * a.length;
-    const int place = it.start + min(i, it.length - 1);
     const float s = a.scale ? a.scale[it.adapter] : 1.0f;
-    v4f acc[4];
+    // (what is there already is requested first: it has the longest way)
+    float *const y = a.out + (size_t)it.vector * a.length;
+    auto value_at = [&](int t) { return r0 + (TURNED ? 16 * kb + 4 * t : 16 * t + 4 * kb); };
+    v4f before[4], acc[4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) acc[t] = v4f{0, 0, 0, 0};
+    for (int t = 0; t < 4; ++t) {
+        before[t] = load4_of<VEC>(y, value_at(t), a.length);
+        acc[t] = v4f{0, 0, 0, 0};
+    }
     for (int rt = 0; rt < a.ranks; ++rt) {
         if constexpr (TURNED) {
             // summand 4 e + kb; tile t has the values r0 + 4 i + t
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int j = rt * 16 + 4 * e + kb;
-                const float u = down1_at(a.parts, a.slices, a.order.batch, a.ranks, place, rt, 4 * e + kb);
+                const float u = down1_at(a.parts, a.slices, a.order.batch, a.ranks, it.vector, rt, 4 * e + kb);
                 const v4f w = j < a.rank ? load4_of<VEC>(M + (size_t)j * a.length, r0 + 4 * i, a.length) : v4f{0, 0, 0, 0};
 #pragma unroll
                 for (int t = 0; t < 4; ++t) acc[t] = mfma(w[t], u, acc[t]);
             }
         } else {
             // summand 4 kb + e; tile t has the values r0 + 16 t + i
-            const v4f u = down_at(a.parts, a.slices, a.order.batch, a.ranks, place, rt, kb) * s;
+            const v4f u = down_at(a.parts, a.slices, a.order.batch, a.ranks, it.vector, rt, kb) * s;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const int r = r0 + 16 * t + i;
@@ -295,13 +358,11 @@ __global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
         }
     }
     if (i >= it.length) return;
-    float *const y = a.out + (size_t)a.order.vector(place) * a.length;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        const int r = r0 + (TURNED ? 16 * kb + 4 * t : 16 * t + 4 * kb);
         v4f v = acc[t];
         if constexpr (TURNED) v = v4f{acc[0][t], acc[1][t], acc[2][t], acc[3][t]};
-        store4_of<VEC>(y, r, a.length, load4_of<VEC>(y, r, a.length) + v);
+        store4_of<VEC>(y, value_at(t), a.length, before[t] + v);
     }
 }
 
@@ -322,24 +383,37 @@ __global__ __launch_bounds__(kOuterWaves * 64) void k_adapter_outer(const OuterA
     __shared__ v4f s_part[kOuterWaves - 1][RT * 4][64];
     const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
     const int k = blockIdx.y, rt0 = blockIdx.z * RT, c = blockIdx.x * 64 + 4 * i;
-    int start, end;
-    a.order.segment(k, &start, &end);
+    const Order::Segment seg = a.order.segment(k, lane);
     v4f acc[RT][4];
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int q = 0; q < 4; ++q) acc[t][q] = v4f{0, 0, 0, 0};
-    for (int p0 = start + 4 * wave; p0 < end; p0 += 4 * kOuterWaves) {
-        const int place = p0 + kb;
-        const bool live = place < end;
-        const v4f v = live ? load4_of<VEC>(a.V + (size_t)a.order.vector(place) * a.length, c, a.length) : v4f{0, 0, 0, 0};
+    // (several requests of vectors at once: their numbers first, then what depends on them)
+    constexpr int AT_ONCE = 4;
+    for (int p0 = 4 * wave; p0 < seg.length; p0 += AT_ONCE * 4 * kOuterWaves) {
+        int n[AT_ONCE];
+        v4f v[AT_ONCE];
+        float u[AT_ONCE][RT];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            float u = 0.0f;
-            if (live && rt0 + t < a.ranks) u = down1_at(a.parts, a.slices, a.order.batch, a.ranks, place, rt0 + t, i);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) acc[t][q] = mfma(u, v[q], acc[t][q]);
+        for (int x = 0; x < AT_ONCE; ++x) {
+            const int p = p0 + x * 4 * kOuterWaves + kb;
+            n[x] = seg.vector(min(p, seg.length - 1));
+            if (p >= seg.length) n[x] = -1;
         }
+#pragma unroll
+        for (int x = 0; x < AT_ONCE; ++x) {
+            v[x] = n[x] >= 0 ? load4_of<VEC>(a.V + (size_t)n[x] * a.length, c, a.length) : v4f{0, 0, 0, 0};
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+                u[x][t] = n[x] >= 0 && rt0 + t < a.ranks ? down1_at(a.parts, a.slices, a.order.batch, a.ranks, n[x], rt0 + t, i) : 0.0f;
+        }
+#pragma unroll
+        for (int x = 0; x < AT_ONCE; ++x)
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc[t][q] = mfma(u[x][t], v[x][q], acc[t][q]);
     }
     if (wave > 0) {
 #pragma unroll
@@ -383,7 +457,7 @@ AdapterPlan adapter_plan(const Layout &L, const pb_adapters &ad, int batch, bool
     // parts of the sums: about two workgroups per compute unit, each wave with 64 summands or more
     const int most = L.rows > L.cols ? L.rows : L.cols;
     int slices = 512 / (p.items * ((p.ranks + 3) / 4));
-    if (slices > (most + 255) / 256) slices = (most + 255) / 256;
+    if (slices > (most + 64 * kDownWaves - 1) / (64 * kDownWaves)) slices = (most + 64 * kDownWaves - 1) / (64 * kDownWaves);
     p.slices = slices < 1 ? 1 : (slices > 16 ? 16 : slices);
     auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
     const size_t down = up((size_t)p.slices * batch * p.ranks * 64);
@@ -396,11 +470,11 @@ AdapterPlan adapter_plan(const Layout &L, const pb_adapters &ad, int batch, bool
     return p;
 }
 
-static Order order_of(const AdapterPlan &p, bool indexed, int batch, void *workspace)
+static Order order_of(const AdapterPlan &p, const pb_adapters &ad, const int32_t *index, int batch, void *workspace)
 {
     char *const ws = static_cast<char *>(workspace);
-    Order o = {nullptr, nullptr, nullptr, nullptr, batch};
-    if (indexed) {
+    Order o = {index, nullptr, nullptr, nullptr, nullptr, batch, ad.count};
+    if (index && batch > kListed) {
         o.order = reinterpret_cast<const int *>(ws);
         o.items = reinterpret_cast<const Item *>(ws + p.items_off);
         o.counts = reinterpret_cast<const int *>(ws + p.counts_off);
@@ -411,7 +485,7 @@ static Order order_of(const AdapterPlan &p, bool indexed, int batch, void *works
 
 int launch_adapter_order(const AdapterPlan &p, const pb_adapters &ad, const int32_t *index, int batch, void *workspace, hipStream_t st)
 {
-    if (!index) return 0;
+    if (!index || batch <= kListed) return 0;
     char *const ws = static_cast<char *>(workspace);
     hipLaunchKernelGGL(k_adapter_order, dim3(1), dim3(kOrderThreads), 0, st, index, batch, ad.count, reinterpret_cast<int *>(ws),
                        reinterpret_cast<Item *>(ws + p.items_off), reinterpret_cast<int *>(ws + p.counts_off),
@@ -444,7 +518,7 @@ static const void *down_kernel(int rt)
 }
 static int ranks_at_once(const AdapterPlan &p) { return p.ranks >= 3 ? 4 : p.ranks; }
 
-int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, bool indexed, const float *X, const float *dY, int batch,
+int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, const float *X, const float *dY, int batch,
                         void *workspace, hipStream_t st)
 {
     char *const ws = static_cast<char *>(workspace);
@@ -453,18 +527,18 @@ int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layou
     return by_type(ad.type, [&](auto type) {
         typedef decltype(type) T;
         DownArgs a;
-        a.order = order_of(p, indexed, batch, workspace);
+        a.order = order_of(p, ad, index, batch, workspace);
         a.rank = ad.rank; a.ranks = p.ranks; a.slices = p.slices;
         int err = 0;
         if (X) {
             a.M = ad.A; a.scale = nullptr; a.V = X; a.length = L.cols;
             a.out = reinterpret_cast<float *>(ws + p.u_off);
-            err = launch(L.cols % 4 ? down_kernel<T, false, false>(rt) : down_kernel<T, false, true>(rt), grid, 256, &a, st);
+            err = launch(L.cols % 4 ? down_kernel<T, false, false>(rt) : down_kernel<T, false, true>(rt), grid, kDownWaves * 64, &a, st);
         }
         if (!err && dY) {
             a.M = ad.B; a.scale = ad.scale; a.V = dY; a.length = L.rows;
             a.out = reinterpret_cast<float *>(ws + p.t_off);
-            err = launch(L.rows % 4 ? down_kernel<T, true, false>(rt) : down_kernel<T, true, true>(rt), grid, 256, &a, st);
+            err = launch(L.rows % 4 ? down_kernel<T, true, false>(rt) : down_kernel<T, true, true>(rt), grid, kDownWaves * 64, &a, st);
         }
         return err;
     });
@@ -479,11 +553,11 @@ static const void *up_kernel(bool vec, bool rank4)
                : reinterpret_cast<const void *>(k_adapter_up<T, false, false, false>);
 }
 
-int launch_adapter_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, bool indexed, int batch, float *Y, void *workspace,
+int launch_adapter_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, int batch, float *Y, void *workspace,
                       hipStream_t st)
 {
     UpArgs a;
-    a.order = order_of(p, indexed, batch, workspace);
+    a.order = order_of(p, ad, index, batch, workspace);
     a.M = ad.B; a.scale = ad.scale; a.parts = reinterpret_cast<const float *>(static_cast<char *>(workspace) + p.u_off); a.out = Y;
     a.length = L.rows; a.rank = ad.rank; a.ranks = p.ranks; a.slices = p.slices;
     return by_type(ad.type, [&](auto type) {
@@ -501,12 +575,12 @@ static const void *outer_kernel(bool vec, bool rank4)
                : reinterpret_cast<const void *>(k_adapter_outer<true, false, false, RT>);
 }
 
-int launch_adapter_grads(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, bool indexed, const float *X, const float *dY, int batch,
+int launch_adapter_grads(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, const float *X, const float *dY, int batch,
                          float *dX, float *dA, float *dB, void *workspace, hipStream_t st)
 {
     char *const ws = static_cast<char *>(workspace);
     const float *const u = reinterpret_cast<const float *>(ws + p.u_off), *const t = reinterpret_cast<const float *>(ws + p.t_off);
-    const Order order = order_of(p, indexed, batch, workspace);
+    const Order order = order_of(p, ad, index, batch, workspace);
     const bool rank4 = ad.rank % 4 == 0;
     int err = 0;
     if (dX) {

@@ -463,13 +463,13 @@ int pb_matmul_adapters(const void *packed, const float *scales, const pb_desc *d
     const pb::AdapterPlan p = pb::adapter_plan(L, *adapters, batch, index != nullptr);
     void *const ws = static_cast<char *>(workspace) + adapters_off(L, batch);
     int err = pb::launch_adapter_order(p, *adapters, index, batch, ws, st);
-    if (!err) err = pb::launch_adapter_down(p, *adapters, L, index != nullptr, X, nullptr, batch, ws, st);
+    if (!err) err = pb::launch_adapter_down(p, *adapters, L, index, X, nullptr, batch, ws, st);
     if (err) return hip_status(err);
     pb::Epilogue ep;
     ep.bias = bias;
     rc = matmul_common(packed, scales, d, bits_used, X, d->cols, nullptr, 0, batch, Y, nullptr, workspace, stream, ep, false, true);
     if (rc != PB_OK) return rc;
-    return hip_status(pb::launch_adapter_up(p, *adapters, L, index != nullptr, batch, Y, ws, st));
+    return hip_status(pb::launch_adapter_up(p, *adapters, L, index, batch, Y, ws, st));
 }
 
 int pb_matmul_adapters_grad(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *X, const float *dY,
@@ -488,10 +488,10 @@ int pb_matmul_adapters_grad(const void *packed, const float *scales, const pb_de
     void *const ws = static_cast<char *>(workspace) + adapters_off(L, batch);
     int err = pb::launch_adapter_order(p, *adapters, index, batch, ws, st);
     // (u is needed for dB, t for dA and dX)
-    if (!err) err = pb::launch_adapter_down(p, *adapters, L, index != nullptr, dB ? X : nullptr, dX || dA ? dY : nullptr, batch, ws, st);
+    if (!err) err = pb::launch_adapter_down(p, *adapters, L, index, dB ? X : nullptr, dX || dA ? dY : nullptr, batch, ws, st);
     if (!err && dX)
         err = pb::launch_grad(static_cast<const uint32_t *>(packed), scales, L, bits_used, dY, nullptr, batch, dX, workspace, st);
-    if (!err) err = pb::launch_adapter_grads(p, *adapters, L, index != nullptr, X, dY, batch, dX, dA, dB, ws, st);
+    if (!err) err = pb::launch_adapter_grads(p, *adapters, L, index, X, dY, batch, dX, dA, dB, ws, st);
     return hip_status(err);
 }
 

@@ -87,16 +87,16 @@ struct AdapterPlan {
     size_t items_off, counts_off, starts_off, u_off, t_off, bytes;
 };
 AdapterPlan adapter_plan(const Layout &L, const pb_adapters &ad, int batch, bool indexed);
-// The order of the vectors (by adapter) and its tiles; nothing to do without an index
+// The order of the vectors (by adapter) and its tiles; nothing to do without an index or for few vectors
 int launch_adapter_order(const AdapterPlan &p, const pb_adapters &ad, const int32_t *index, int batch, void *workspace, hipStream_t st);
 // u = A_k x (and t = scale_k B_k^T dY, if dY is given) of the ordered vectors, in parts
-int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, bool indexed, const float *X, const float *dY, int batch,
+int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, const float *X, const float *dY, int batch,
                         void *workspace, hipStream_t st);
 // Y += scale_k B_k u
-int launch_adapter_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, bool indexed, int batch, float *Y, void *workspace,
+int launch_adapter_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, int batch, float *Y, void *workspace,
                       hipStream_t st);
 // dX += A_k^T t (if dX is given), dA_k = sum t x^T, dB_k = scale_k sum dy u^T (where given)
-int launch_adapter_grads(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, bool indexed, const float *X, const float *dY, int batch,
+int launch_adapter_grads(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, const float *X, const float *dY, int batch,
                          float *dX, float *dA, float *dB, void *workspace, hipStream_t st);
 
 }  // namespace pb
