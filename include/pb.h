@@ -261,7 +261,8 @@ int pb_lstm_cell(const void *packed, const float *scales, const pb_desc *d, int 
  *   H     [batch][F], written
  *   pre   [batch][2F] or NULL: the pre-activations [g ; u], written (what the backward pass needs)
  *   workspace: pb_workspace_bytes(d, batch) bytes, overwritten
- * No output may overlap another one or an input.  PB_EINVAL if rows is odd. */
+ * No output may overlap another one or an input.  PB_EINVAL if rows is odd.  With PB_LAYOUT_TILE16_GATES_V1 (F even) the product and
+ * the gate are one launch where there are few vectors: its row tiles hold rows r, F/2 + r, F + r, 3F/2 + r next to each other, the gates and the values of two units. */
 typedef enum pb_gate { PB_GATE_SIGMOID = 0, PB_GATE_SILU = 1, PB_GATE_GELU = 2, PB_GATE_RELU = 3 } pb_gate;
 int pb_gated_linear(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *X, int batch,
                     const float *bias, int gate, float *H, float *pre, void *workspace, void *stream);

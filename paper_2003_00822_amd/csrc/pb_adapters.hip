@@ -63,7 +63,7 @@ __device__ __forceinline__ void store4_of(float *p, int at, int length, v4f v)
 __device__ __forceinline__ v4f mfma(float a, float b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 // ---- the order of the vectors ----
-struct Item { int adapter, start, length, pad; };     // places start .. start + length of the order
+struct Item { int adapter, length, vector[16]; };
 
 // The r-th of the lanes that are set in `mask`, in lane r
 __device__ __forceinline__ int lanes_in_order(unsigned long long mask, int lane)
@@ -108,9 +108,12 @@ struct Order {
             return i * 16 < batch;
         }
         if (order) {
-            if (i >= counts[0]) return false;
-            const Item it = items[i];
-            *t = {it.adapter, it.length, order[it.start + min(lane & 15, it.length - 1)]};
+            // (all read at once; items that are none hold anything)
+            const int tiles = counts[0], length = items[i].length, vector = items[i].vector[lane & 15];
+            *t = {items[i].adapter, length, vector};
+            if (i >= tiles) return false;
+            const int last = __shfl(vector, length - 1);
+            if ((lane & 15) >= length) t->vector = last;
             return true;
         }
         const int key = key_of(lane);
@@ -211,7 +214,12 @@ __global__ __launch_bounds__(kOrderThreads) void k_adapter_order(const int32_t *
         if (k < 0) continue;
         const int start = (int)(s_first[k] & 0xFFFFu), at = start + place[i];
         order[at] = n;
-        if (place[i] % 16 == 0) items[(s_first[k] >> 16) + place[i] / 16] = {k, at, min(16, s_count[k] - place[i]), 0};
+        Item *const it = items + (s_first[k] >> 16) + place[i] / 16;
+        it->vector[place[i] % 16] = n;
+        if (place[i] % 16 == 0) {
+            it->adapter = k;
+            it->length = min(16, s_count[k] - place[i]);
+        }
     }
 }
 
@@ -228,19 +236,16 @@ struct DownArgs {
 //   TURNED: the summands are the rows of the matrix (B: [length][rank]), else its columns (A: [rank][length])
 constexpr int kDownWaves = 8;
 template <typename T, bool TURNED, bool VEC, int RT>
-__global__ __launch_bounds__(kDownWaves * 64) void k_adapter_down(const DownArgs a)
+__device__ __forceinline__ void adapter_down(const DownArgs &a, int rt0, v4f (*s_part)[RT][64])
 {
-    __shared__ v4f s_part[kDownWaves - 1][RT][64];
     const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
     Order::Tile it;
     if (!a.order.tile(blockIdx.x, lane, &it)) return;
     const T *const M = static_cast<const T *>(a.M) + (size_t)it.adapter * a.rank * a.length;
     const float *const x = a.V + (size_t)it.vector * a.length;
-    const int rt0 = blockIdx.z * RT;
     v4f acc[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[t] = v4f{0, 0, 0, 0};
-#pragma unroll 2
     for (int c0 = (blockIdx.y * kDownWaves + wave) * 64; c0 < a.length; c0 += a.slices * kDownWaves * 64) {
         v4f v[4], w[4][RT];
 #pragma unroll
@@ -290,6 +295,15 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_adapter_down(const DownArgs
         *reinterpret_cast<v4f *>(a.out + (((size_t)blockIdx.y * a.order.batch + it.vector) * a.ranks + rt0 + t) * 16 + 4 * kb) = v;
     }
 }
+// u, t or both
+template <typename T, bool VEC_X, bool VEC_DY, int RT>
+__global__ __launch_bounds__(kDownWaves * 64) void k_adapter_down(const DownArgs u, const DownArgs t)
+{
+    __shared__ v4f s_part[kDownWaves - 1][RT][64];
+    const int z = blockIdx.z * RT;
+    if (u.V && z < u.ranks) adapter_down<T, false, VEC_X, RT>(u, z, s_part);
+    else adapter_down<T, true, VEC_DY, RT>(t, u.V ? z - (u.ranks + RT - 1) / RT * RT : z, s_part);
+}
 // Ranks 4 part .. 4 part + 3 of rank tile `rt` of a vector: the slices added up in their order
 __device__ __forceinline__ v4f down_at(const float *parts, int slices, int batch, int ranks, int vector, int rt, int part)
 {
@@ -313,56 +327,90 @@ struct UpArgs {
     const float *scale;       // (Y only)
     const float *parts;       // u or t
     float *out;               // [batch][length]
-    int length, rank, ranks, slices;
+    int length, rank, ranks, slices, blocks;
 };
-// A wave does 64 values of the tile's vectors.  TURNED: M is A [rank][length], else B [length][rank]
-template <typename T, bool TURNED, bool VEC, bool RANK4>
+// A wave does `blocks` times 64 values of the tile's vectors.  RT rank tiles at once.  TURNED: M is A [rank][length], else B [length][rank]
+template <typename T, bool TURNED, bool VEC, bool RANK4, int RT>
 __global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
 {
     const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
-    const int r0 = (blockIdx.x * 4 + wave) * 64;
+    const int first = (blockIdx.x * 4 + wave) * a.blocks * 64, end = min(first + a.blocks * 64, a.length);
     Order::Tile it;
-    if (r0 >= a.length || !a.order.tile(blockIdx.y, lane, &it)) return;
+    if (first >= a.length || !a.order.tile(blockIdx.y, lane, &it)) return;
     const T *const M = static_cast<const T *>(a.M) + (size_t)it.adapter * a.rank * a.length;
     const float s = a.scale ? a.scale[it.adapter] : 1.0f;
-    // (what is there already is requested first: it has the longest way)
     float *const y = a.out + (size_t)it.vector * a.length;
-    auto value_at = [&](int t) { return r0 + (TURNED ? 16 * kb + 4 * t : 16 * t + 4 * kb); };
-    v4f before[4], acc[4];
+    // a lane's values: four times four next to each other
+    auto value_at = [&](int r0, int t) { return r0 + 16 * t + 4 * kb; };
+    // summands of rank tile t: 4 e + kb (TURNED), 4 kb + e
+    float u[RT][4];
+    auto load_u = [&](int rt0) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        before[t] = load4_of<VEC>(y, value_at(t), a.length);
-        acc[t] = v4f{0, 0, 0, 0};
-    }
-    for (int rt = 0; rt < a.ranks; ++rt) {
-        if constexpr (TURNED) {
-            // summand 4 e + kb; tile t has the values r0 + 4 i + t
+        for (int t = 0; t < RT; ++t) {
+            if (rt0 + t < a.ranks) {
+                if constexpr (TURNED) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int j = rt * 16 + 4 * e + kb;
-                const float u = down1_at(a.parts, a.slices, a.order.batch, a.ranks, it.vector, rt, 4 * e + kb);
-                const v4f w = j < a.rank ? load4_of<VEC>(M + (size_t)j * a.length, r0 + 4 * i, a.length) : v4f{0, 0, 0, 0};
+                    for (int e = 0; e < 4; ++e) u[t][e] = down1_at(a.parts, a.slices, a.order.batch, a.ranks, it.vector, rt0 + t, 4 * e + kb);
+                } else {
+                    const v4f v = down_at(a.parts, a.slices, a.order.batch, a.ranks, it.vector, rt0 + t, kb) * s;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) acc[t] = mfma(w[t], u, acc[t]);
-            }
-        } else {
-            // summand 4 kb + e; tile t has the values r0 + 16 t + i
-            const v4f u = down_at(a.parts, a.slices, a.order.batch, a.ranks, it.vector, rt, kb) * s;
+                    for (int e = 0; e < 4; ++e) u[t][e] = v[e];
+                }
+            } else {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int r = r0 + 16 * t + i;
-                const v4f w = r < a.length ? load4_of<RANK4>(M + (size_t)r * a.rank, rt * 16 + 4 * kb, a.rank) : v4f{0, 0, 0, 0};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[t] = mfma(w[e], u[e], acc[t]);
+                for (int e = 0; e < 4; ++e) u[t][e] = 0.0f;
             }
         }
-    }
-    if (i >= it.length) return;
+    };
+    v4f before[4];
+    auto load_before = [&](int r0) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        v4f v = acc[t];
-        if constexpr (TURNED) v = v4f{acc[0][t], acc[1][t], acc[2][t], acc[3][t]};
-        store4_of<VEC>(y, value_at(t), a.length, before[t] + v);
+        for (int t = 0; t < 4; ++t) before[t] = load4_of<VEC>(y, value_at(r0, t), end);
+    };
+    load_before(first);
+    load_u(0);
+    for (int r0 = first; r0 < end; r0 += 64) {
+        v4f acc[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[t] = v4f{0, 0, 0, 0};
+        for (int rt0 = 0; rt0 < a.ranks; rt0 += RT) {
+            if (a.ranks > RT) load_u(rt0);
+            v4f w[RT][4];
+#pragma unroll
+            for (int x = 0; x < RT; ++x)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    w[x][t] = v4f{0, 0, 0, 0};
+                    if constexpr (TURNED) {      // t: summand 4 t + kb, four values (in the order in which a lane's results then are four and four)
+                        const int j = (rt0 + x) * 16 + 4 * t + kb;
+                        if (j < a.rank) w[x][t] = load4_of<VEC>(M + (size_t)j * a.length, r0 + 16 * (i & 3) + 4 * (i >> 2), a.length);
+                    } else {                     // t: value r0 + 16 t + i, the summands 4 kb .. 4 kb + 3
+                        const int r = r0 + 16 * t + i;
+                        if (r < a.length) w[x][t] = load4_of<RANK4>(M + (size_t)r * a.rank, (rt0 + x) * 16 + 4 * kb, a.rank);
+                    }
+                }
+#pragma unroll
+            for (int x = 0; x < RT; ++x)
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (TURNED) acc[e] = mfma(w[x][t][e], u[x][t], acc[e]);
+                        else acc[t] = mfma(w[x][t][e], u[x][e], acc[t]);
+                    }
+        }
+        v4f now[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) now[t] = before[t];
+        if (r0 + 64 < end) load_before(r0 + 64);
+        if (i < it.length) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                v4f v = acc[t];
+                if constexpr (TURNED) v = v4f{acc[0][t], acc[1][t], acc[2][t], acc[3][t]};
+                store4_of<VEC>(y, value_at(r0, t), end, now[t] + v);
+            }
+        }
     }
 }
 
@@ -378,11 +426,10 @@ struct OuterArgs {
 constexpr int kOuterWaves = 8;
 // A workgroup does 64 columns (rows) and RT rank tiles of an adapter; its waves take every eighth four of the adapter's vectors.
 template <bool TURNED, bool VEC, bool RANK4, int RT>
-__global__ __launch_bounds__(kOuterWaves * 64) void k_adapter_outer(const OuterArgs a)
+__device__ __forceinline__ void adapter_outer(const OuterArgs &a, int block, v4f (*s_part)[RT * 4][64])
 {
-    __shared__ v4f s_part[kOuterWaves - 1][RT * 4][64];
     const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
-    const int k = blockIdx.y, rt0 = blockIdx.z * RT, c = blockIdx.x * 64 + 4 * i;
+    const int k = blockIdx.y, rt0 = blockIdx.z * RT, c = block * 64 + 4 * i;
     const Order::Segment seg = a.order.segment(k, lane);
     v4f acc[RT][4];
 #pragma unroll
@@ -390,7 +437,7 @@ __global__ __launch_bounds__(kOuterWaves * 64) void k_adapter_outer(const OuterA
 #pragma unroll
         for (int q = 0; q < 4; ++q) acc[t][q] = v4f{0, 0, 0, 0};
     // (several requests of vectors at once: their numbers first, then what depends on them)
-    constexpr int AT_ONCE = 4;
+    constexpr int AT_ONCE = RT == 1 ? 8 : 4;
     for (int p0 = 4 * wave; p0 < seg.length; p0 += AT_ONCE * 4 * kOuterWaves) {
         int n[AT_ONCE];
         v4f v[AT_ONCE];
@@ -444,6 +491,16 @@ __global__ __launch_bounds__(kOuterWaves * 64) void k_adapter_outer(const OuterA
                     store4_of<VEC>(a.out + ((size_t)k * a.rank + j + e) * a.length, c, a.length, v4f{acc[t][0][e], acc[t][1][e], acc[t][2][e], acc[t][3][e]});
         }
     }
+}
+
+// dA, dB or both
+template <bool VEC_X, bool VEC_DY, bool RANK4, int RT>
+__global__ __launch_bounds__(kOuterWaves * 64) void k_adapter_outer(const OuterArgs A, const OuterArgs B)
+{
+    __shared__ v4f s_part[kOuterWaves - 1][RT * 4][64];
+    const int block = blockIdx.x, of_A = A.out ? (A.length + 63) / 64 : 0;
+    if (block < of_A) adapter_outer<false, VEC_X, RANK4, RT>(A, block, s_part);
+    else adapter_outer<true, VEC_DY, RANK4, RT>(B, block - of_A, s_part);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -509,105 +566,109 @@ static int launch(const void *fn, dim3 grid, int threads, void *args, hipStream_
     const hipError_t e = hipLaunchKernel(fn, grid, dim3((unsigned)threads), list, 0, st);
     return (int)(e != hipSuccess ? e : hipGetLastError());
 }
-template <typename T, bool TURNED, bool VEC>
-static const void *down_kernel(int rt)
+// The kernel for two truth values
+template <template <bool, bool> class K>
+static const void *by_two(bool a, bool b)
 {
-    if (rt == 1) return reinterpret_cast<const void *>(k_adapter_down<T, TURNED, VEC, 1>);
-    if (rt == 2) return reinterpret_cast<const void *>(k_adapter_down<T, TURNED, VEC, 2>);
-    return reinterpret_cast<const void *>(k_adapter_down<T, TURNED, VEC, 4>);
+    if (a) return b ? K<true, true>::fn() : K<true, false>::fn();
+    return b ? K<false, true>::fn() : K<false, false>::fn();
 }
-static int ranks_at_once(const AdapterPlan &p) { return p.ranks >= 3 ? 4 : p.ranks; }
+template <typename T, int RT>
+struct Down {
+    template <bool X, bool DY>
+    struct K { static const void *fn() { return reinterpret_cast<const void *>(k_adapter_down<T, X, DY, RT>); } };
+};
+template <typename T, bool TURNED, int RT>
+struct Up {
+    // (the rank of A's rows does not matter)
+    template <bool VEC, bool RANK4>
+    struct K { static const void *fn() { return reinterpret_cast<const void *>(k_adapter_up<T, TURNED, VEC, TURNED || RANK4, RT>); } };
+};
+template <bool RANK4, int RT>
+struct Outer {
+    template <bool X, bool DY>
+    struct K { static const void *fn() { return reinterpret_cast<const void *>(k_adapter_outer<X, DY, RANK4, RT>); } };
+};
+static int launch_two(const void *fn, dim3 grid, int threads, void *first, void *second, hipStream_t st)
+{
+    void *list[] = {first, second};
+    const hipError_t e = hipLaunchKernel(fn, grid, dim3((unsigned)threads), list, 0, st);
+    return (int)(e != hipSuccess ? e : hipGetLastError());
+}
 
 int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, const float *X, const float *dY, int batch,
                         void *workspace, hipStream_t st)
 {
     char *const ws = static_cast<char *>(workspace);
-    const int rt = ranks_at_once(p);
-    const dim3 grid((unsigned)p.items, (unsigned)p.slices, (unsigned)((p.ranks + rt - 1) / rt));
+    const int rt = p.ranks >= 3 ? 4 : p.ranks, z = (p.ranks + rt - 1) / rt;
+    DownArgs u, t;
+    u.order = order_of(p, ad, index, batch, workspace);
+    u.rank = ad.rank; u.ranks = p.ranks; u.slices = p.slices;
+    t = u;
+    u.M = ad.A; u.scale = nullptr; u.V = X; u.length = L.cols; u.out = reinterpret_cast<float *>(ws + p.u_off);
+    t.M = ad.B; t.scale = ad.scale; t.V = dY; t.length = L.rows; t.out = reinterpret_cast<float *>(ws + p.t_off);
+    const bool vx = L.cols % 4 == 0, vy = L.rows % 4 == 0;
     return by_type(ad.type, [&](auto type) {
         typedef decltype(type) T;
-        DownArgs a;
-        a.order = order_of(p, ad, index, batch, workspace);
-        a.rank = ad.rank; a.ranks = p.ranks; a.slices = p.slices;
-        int err = 0;
-        if (X) {
-            a.M = ad.A; a.scale = nullptr; a.V = X; a.length = L.cols;
-            a.out = reinterpret_cast<float *>(ws + p.u_off);
-            err = launch(L.cols % 4 ? down_kernel<T, false, false>(rt) : down_kernel<T, false, true>(rt), grid, kDownWaves * 64, &a, st);
-        }
-        if (!err && dY) {
-            a.M = ad.B; a.scale = ad.scale; a.V = dY; a.length = L.rows;
-            a.out = reinterpret_cast<float *>(ws + p.t_off);
-            err = launch(L.rows % 4 ? down_kernel<T, true, false>(rt) : down_kernel<T, true, true>(rt), grid, kDownWaves * 64, &a, st);
-        }
-        return err;
+        const void *fn = rt == 1 ? by_two<Down<T, 1>::template K>(vx, vy)
+                                 : (rt == 2 ? by_two<Down<T, 2>::template K>(vx, vy) : by_two<Down<T, 4>::template K>(vx, vy));
+        return launch_two(fn, dim3((unsigned)p.items, (unsigned)p.slices, (unsigned)(z * ((X ? 1 : 0) + (dY ? 1 : 0)))), kDownWaves * 64, &u, &t, st);
     });
 }
 
-template <typename T, bool TURNED>
-static const void *up_kernel(bool vec, bool rank4)
+// Y += ... with B (TURNED: dX += ... with A)
+template <bool TURNED>
+static int launch_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, int batch, float *out, void *workspace,
+                     hipStream_t st)
 {
-    if (TURNED || rank4) return vec ? reinterpret_cast<const void *>(k_adapter_up<T, TURNED, true, true>)
-                                    : reinterpret_cast<const void *>(k_adapter_up<T, TURNED, false, true>);
-    return vec ? reinterpret_cast<const void *>(k_adapter_up<T, false, true, false>)
-               : reinterpret_cast<const void *>(k_adapter_up<T, false, false, false>);
+    UpArgs a;
+    a.order = order_of(p, ad, index, batch, workspace);
+    a.M = TURNED ? ad.A : ad.B;
+    a.scale = TURNED ? nullptr : ad.scale;
+    a.parts = reinterpret_cast<const float *>(static_cast<char *>(workspace) + (TURNED ? p.t_off : p.u_off));
+    a.out = out;
+    a.length = TURNED ? L.cols : L.rows;
+    a.rank = ad.rank; a.ranks = p.ranks; a.slices = p.slices;
+    // Blocks of 64 values per wave: one while that leaves the chip room, up to four (a wave finds its tile and its ranks once)
+    const long long waves = (long long)((a.length + 63) / 64) * p.items;
+    a.blocks = waves < 2 * 4096 ? 1 : (waves < 4 * 4096 ? 2 : 4);
+    const int rt = p.ranks >= 3 ? 4 : p.ranks;
+    const bool vec = a.length % 4 == 0, rank4 = TURNED || ad.rank % 4 == 0;
+    return by_type(ad.type, [&](auto type) {
+        typedef decltype(type) T;
+        const void *fn = rt == 1 ? by_two<Up<T, TURNED, 1>::template K>(vec, rank4)
+                                 : (rt == 2 ? by_two<Up<T, TURNED, 2>::template K>(vec, rank4) : by_two<Up<T, TURNED, 4>::template K>(vec, rank4));
+        return launch(fn, dim3((unsigned)((a.length + 256 * a.blocks - 1) / (256 * a.blocks)), (unsigned)p.items), 256, &a, st);
+    });
 }
 
 int launch_adapter_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, int batch, float *Y, void *workspace,
                       hipStream_t st)
 {
-    UpArgs a;
-    a.order = order_of(p, ad, index, batch, workspace);
-    a.M = ad.B; a.scale = ad.scale; a.parts = reinterpret_cast<const float *>(static_cast<char *>(workspace) + p.u_off); a.out = Y;
-    a.length = L.rows; a.rank = ad.rank; a.ranks = p.ranks; a.slices = p.slices;
-    return by_type(ad.type, [&](auto type) {
-        return launch(up_kernel<decltype(type), false>(L.rows % 4 == 0, ad.rank % 4 == 0),
-                      dim3((unsigned)((L.rows + 255) / 256), (unsigned)p.items), 256, &a, st);
-    });
-}
-
-template <bool TURNED, int RT>
-static const void *outer_kernel(bool vec, bool rank4)
-{
-    if (!TURNED || rank4) return vec ? reinterpret_cast<const void *>(k_adapter_outer<TURNED, true, true, RT>)
-                                     : reinterpret_cast<const void *>(k_adapter_outer<TURNED, false, true, RT>);
-    return vec ? reinterpret_cast<const void *>(k_adapter_outer<true, true, false, RT>)
-               : reinterpret_cast<const void *>(k_adapter_outer<true, false, false, RT>);
+    return launch_up<false>(p, ad, L, index, batch, Y, workspace, st);
 }
 
 int launch_adapter_grads(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, const float *X, const float *dY, int batch,
                          float *dX, float *dA, float *dB, void *workspace, hipStream_t st)
 {
     char *const ws = static_cast<char *>(workspace);
-    const float *const u = reinterpret_cast<const float *>(ws + p.u_off), *const t = reinterpret_cast<const float *>(ws + p.t_off);
-    const Order order = order_of(p, ad, index, batch, workspace);
-    const bool rank4 = ad.rank % 4 == 0;
-    int err = 0;
     if (dX) {
-        UpArgs a;
-        a.order = order; a.M = ad.A; a.scale = nullptr; a.parts = t; a.out = dX;
-        a.length = L.cols; a.rank = ad.rank; a.ranks = p.ranks; a.slices = p.slices;
-        err = by_type(ad.type, [&](auto type) {
-            return launch(up_kernel<decltype(type), true>(L.cols % 4 == 0, true), dim3((unsigned)((L.cols + 255) / 256), (unsigned)p.items), 256,
-                          &a, st);
-        });
+        const int err = launch_up<true>(p, ad, L, index, batch, dX, workspace, st);
+        if (err) return err;
     }
-    const unsigned z = p.ranks == 1 ? 1u : (unsigned)((p.ranks + 1) / 2);
-    OuterArgs o;
-    o.order = order; o.rank = ad.rank; o.ranks = p.ranks; o.slices = p.slices;
-    if (!err && dA) {
-        o.scale = nullptr; o.parts = t; o.V = X; o.out = dA; o.length = L.cols;
-        const bool vec = L.cols % 4 == 0;
-        err = launch(p.ranks == 1 ? outer_kernel<false, 1>(vec, rank4) : outer_kernel<false, 2>(vec, rank4),
-                     dim3((unsigned)((L.cols + 63) / 64), (unsigned)ad.count, z), kOuterWaves * 64, &o, st);
-    }
-    if (!err && dB) {
-        o.scale = ad.scale; o.parts = u; o.V = dY; o.out = dB; o.length = L.rows;
-        const bool vec = L.rows % 4 == 0;
-        err = launch(p.ranks == 1 ? outer_kernel<true, 1>(vec, rank4) : outer_kernel<true, 2>(vec, rank4),
-                     dim3((unsigned)((L.rows + 63) / 64), (unsigned)ad.count, z), kOuterWaves * 64, &o, st);
-    }
-    return err;
+    if (!dA && !dB) return 0;
+    OuterArgs A, B;
+    A.order = order_of(p, ad, index, batch, workspace);
+    A.rank = ad.rank; A.ranks = p.ranks; A.slices = p.slices;
+    B = A;
+    A.scale = nullptr; A.parts = reinterpret_cast<const float *>(ws + p.t_off); A.V = X; A.out = dA; A.length = L.cols;
+    B.scale = ad.scale; B.parts = reinterpret_cast<const float *>(ws + p.u_off); B.V = dY; B.out = dB; B.length = L.rows;
+    const bool vx = L.cols % 4 == 0, vy = L.rows % 4 == 0, rank4 = ad.rank % 4 == 0;
+    const int rt = p.ranks == 1 ? 1 : 2;
+    const void *fn = rt == 1 ? (rank4 ? by_two<Outer<true, 1>::K>(vx, vy) : by_two<Outer<false, 1>::K>(vx, vy))
+                             : (rank4 ? by_two<Outer<true, 2>::K>(vx, vy) : by_two<Outer<false, 2>::K>(vx, vy));
+    const int blocks = (dA ? (L.cols + 63) / 64 : 0) + (dB ? (L.rows + 63) / 64 : 0);
+    return launch_two(fn, dim3((unsigned)blocks, (unsigned)ad.count, (unsigned)((p.ranks + rt - 1) / rt)), kOuterWaves * 64, &A, &B, st);
 }
 
 }  // namespace pb

@@ -164,7 +164,7 @@ static int matmul_common(const void *packed, const float *scales, const pb_desc 
     pb::Layout L;
     int rc = check_desc(d, &L);
     if (rc != PB_OK) return rc;
-    if (!packed || !X0 || !workspace || (!Y && !A) || (Y && !scales)) return PB_EINVAL;
+    if (!packed || !X0 || !workspace || (!Y && !A && !ep.fused()) || ((Y || ep.fused()) && !scales)) return PB_EINVAL;
     if (bits_used < 1 || bits_used > d->bits) return PB_EINVAL;
     if (batch < 1) return PB_EINVAL;
     if (batch > PB_MAX_BATCH) return PB_ESIZE;
@@ -369,6 +369,12 @@ int pb_gated_linear(const void *packed, const float *scales, const pb_desc *d, i
     if (!aligned16(H) || !aligned16(pre) || !aligned16(workspace)) return PB_EALIGN;
     pb::Epilogue ep;
     ep.bias = bias;
+    if (L.layout == PB_LAYOUT_TILE16_GATES_V1) {       // the gate and the value of a unit meet in a row tile: one launch behind that of the digits
+        ep.gate = gate;
+        ep.h_out = H;
+        ep.pre = reinterpret_cast<float *>(static_cast<char *>(workspace) + pb::ws_gates_off(L, batch));
+        return matmul_common(packed, scales, d, bits_used, X, d->cols, nullptr, 0, batch, pre, nullptr, workspace, stream, ep);
+    }
     const Issuing issuing(workspace);
     float *const to = pre ? pre : reinterpret_cast<float *>(static_cast<char *>(workspace) + pb::ws_gates_off(L, batch));
     rc = matmul_common(packed, scales, d, bits_used, X, d->cols, nullptr, 0, batch, to, nullptr, workspace, stream, ep, false, true);

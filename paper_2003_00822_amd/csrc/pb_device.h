@@ -80,6 +80,12 @@ __device__ __forceinline__ float gate_act(int gate, float v)
     const float s = 1.0f / (1.0f + expf(-t));
     return gate == PB_GATE_SIGMOID ? s : v * s;
 }
+// Gated block on the layout of an LSTM's gates: the four rows of a quad of lanes are the gates of units u and units / 2 + u, then their values.
+// act(g) u of the two units, in the first two lanes.
+__device__ __forceinline__ float gated_quad(int gate, float y)
+{
+    return gate_act(gate, y) * __uint_as_float(dpp_mov<0xEE>(__float_as_uint(y)));
+}
 __device__ __forceinline__ void gate_with_slope(int gate, float v, float *a, float *da)
 {
     if (gate == PB_GATE_RELU) {

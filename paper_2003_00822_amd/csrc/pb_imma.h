@@ -254,10 +254,12 @@ struct I8Args {
     int R;
     double out_scale;
     const uint8_t *wide;                 // beside the digits
+    int gate;                            // (kGated)
 };
 
-// What a kernel does with the sums: store Y (bias and ReLU first), update the LSTM cell, store the sums themselves
-enum { kStore = 0, kCell = 1, kSums = 2 };
+// What a kernel does with the sums: store Y (bias and ReLU first), update the LSTM cell, store the sums themselves, a gated block's
+// act(g) u (k_gated_stream)
+enum { kStore = 0, kCell = 1, kSums = 2, kGated = 3 };
 
 // Whether one of the values of so many quads of vectors needs four digits (the lanes see one chunk each: there are at most 64)
 template <int QUADS>
@@ -340,7 +342,13 @@ __device__ __forceinline__ void finish(const I8Args &a, int lane, int row, bool 
     const bool live = row_ok && n < a.act.batch;
     float y = (float)(v * a.out_scale);
     if (a.bias) y += bias_row;
-    if constexpr (EPI == kCell) {
+    if constexpr (EPI == kGated) {
+        const float h = gated_quad(a.gate, y);
+        if (live) {
+            if (a.Y) a.Y[(size_t)n * a.R + row] = y;
+            if ((lane & 2) == 0) a.h_out[(size_t)n * (a.R / 2) + row] = h;
+        }
+    } else if constexpr (EPI == kCell) {
         float cn, hn;
         lstm_quad(y, lane, c_old, &cn, &hn);
         if ((lane & 3) == 0 && live) {

@@ -90,278 +90,18 @@ template <int ND, int Q, bool IL, int TM, bool FUSED, int EPI, int POLICY, bool 
 __global__ __launch_bounds__(stream_waves(TM) * 64)
 __attribute__((amdgpu_waves_per_eu(stream_waves(TM) / 4, !FUSED && TM == 1 ? 4 : 8))) void k_i8(const I8Args a)
 {
-    constexpr int VPT = 16 / ND;            // vectors per tile of sixteen digit rows
-    constexpr int VPL = 4 / ND;             // vectors per lane of a result: its four registers are the digits of these
-    // four tiles of four digits: tile d is digit d of sixteen vectors.  Else the rows of a tile are, from memory, a digit of four vectors
-    // after the other (four lanes next to each other read 64 bytes in one piece: otherwise a load takes several times as long), and
-    // as staged a digit of one vector after the other.
-    // The digits of one tile are side by side in a register, and the third of four is turned to u ^ 0x80 when they are made: with flags to wait
-    // for and a XOR in the loop, as in PLANES, it was slower than with four digits of every value (977 x 10807, 6 bitlayers, 3 vectors
-    // 8.4 -> 9.1 us, now 8.1; 870 x 9440, 21 vectors 13.2 -> 13.5, now 12.5).  PLAIN: with them all the same, see launch_imma (pb_act_prep
-    // does not know the kernel: two products of 977 x 10807, 3 vectors 14.6 -> 15.5 us).
-    constexpr bool PLANES = !FUSED && TM == 4 && ND == 4;
-    constexpr bool ONES = ND > 1;
-    __shared__ int s_sum[2][TM * 4][64];
-    __shared__ int s_ones[3][64];           // sums of the codes, per row
-    __shared__ double s_z[TM * VPL][64];
-    __shared__ float s_scales[PB_MAX_BITS];
-    extern __shared__ __align__(16) unsigned char stage[];
-    static_assert(sizeof s_sum + ONES * sizeof s_ones + (EPI != kSums) * sizeof s_z + sizeof s_scales == stream_lds(ND, TM, EPI), "LDS");
+#include "pb_i8_stream.inc"
+}
 
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int nwaves = (a.cq + a.chunks_per_wave - 1) / a.chunks_per_wave;   // = blockDim.x / 64
-    const int q0 = wave * a.chunks_per_wave;
-    const int nq = min(a.chunks_per_wave, a.cq - q0);      // >= 1 by construction
-    const int n0 = blockIdx.y * (TM * VPT);
-    const int rt0 = blockIdx.x * a.rounds_per_wg;
-    const int rounds = min(a.rounds_per_wg, a.rt_count - rt0);   // >= 1 by construction
-    const int m = a.m;
-    const int kb = lane >> 4, j = lane & 15;
-
-    // ---- the weight stream: units (round, group of bitlayers, chunk) ----
-    bool merged = EPI != kSums;             // (until the scales are known)
-    struct Unit { int r, f, e, i; };
-    auto group_end = [&](int f) {
-        const int size = merged ? (f == 0 ? 4 * Q : 4 * Q - 2) : (a.pairs_out ? 2 : 1);
-        return min(m, f + size);
-    };
-    // the next unit; true if it belongs to another group of bitlayers
-    auto advance = [&](Unit &u) {
-        if (++u.i < nq) return false;
-        u.i = 0;
-        const int f = u.f;
-        u.f = u.e;
-        if (u.f == m) { u.f = 0; ++u.r; }
-        u.e = group_end(u.f);
-        return u.f != f;
-    };
-    const char *base = reinterpret_cast<const char *>(a.packed) + (size_t)rt0 * a.round_step;
-    const uint32_t avail = (uint32_t)(a.packed_bytes - (size_t)rt0 * a.round_step);
-    // bitlayer of slot 0 of a group: the group starts at slot 0 (even bitlayer 0) or slot 2
-    auto slot0_layer = [](const Unit &u) { return (u.f & ~1) == 0 ? 0 : (u.f & ~1) - 2; };
-    // of the group being requested: the records that the descriptor of a slot shows (an absent slot has none: the load returns
-    // 0 and moves no data); of the group being multiplied: (IL) which of the two bits of a pair's digits belong to it
-    uint32_t records[4 * Q], mask[2 * Q];
-    auto request_group = [&](const Unit &u) {
-        const int l0 = slot0_layer(u);
-#pragma unroll
-        for (int s = 0; s < 4 * Q; ++s) {
-            const int l = l0 + s, lu = l0 + (s & ~1);
-            records[s] = (IL ? lu + 1 >= u.f && lu < u.e : l >= u.f && l < u.e) ? avail : 0u;
-        }
-    };
-    auto multiply_group = [&](const Unit &u) {
-        const int l0 = slot0_layer(u);
-#pragma unroll
-        for (int p = 0; p < 2 * Q; ++p) {
-            const int l = l0 + 2 * p;
-            mask[p] = (l >= u.f && l < u.e ? 0xAAAAAAAAu : 0u) | (l + 1 >= u.f && l + 1 < u.e ? 0x55555555u : 0u);
-        }
-    };
-    u32x4 ring[2][4 * Q];
-    auto issue = [&](u32x4 (&dst)[4 * Q], const Unit &u) {
-        const bool ok = u.r < rounds;
-        const uint32_t off = (uint32_t)u.r * a.round_step + (uint32_t)(q0 + u.i) * 1024u + (uint32_t)slot0_layer(u) * a.layer_step;
-#pragma unroll
-        for (int s = 0; s < 4 * Q; ++s) {
-            const __amdgpu_buffer_rsrc_t rs =
-                __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, ok ? (int)records[s] : 0, 0x00020000);
-            dst[s] = __builtin_amdgcn_raw_buffer_load_b128(rs, lane * 16, (int)(off + (uint32_t)s * a.layer_step), POLICY);
-        }
-    };
-    // Layer scales, lane i holds scales[i] and the next one (range-checked: none without scales)
-    float scv = 0.0f, scn = 0.0f;
-    {
-        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.scales), 0,
-                                                                            a.scales ? m * 4 : 0, 0x00020000);
-        scv = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, lane * 4, 0, 0));
-        scn = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, lane * 4 + 4, 0, 0));
-    }
-    uint32_t wide_here = 0;
-    if constexpr (PLANES || PLAIN) wide_here = load_wide<TM * VPT / 4>(a, n0 / 4, lane);
-    Unit ld = {0, 0, group_end(0), 0};
-    request_group(ld);
-
-    for (int i = threadIdx.x; i < 2 * TM * 4 * 64; i += nwaves * 64) (&s_sum[0][0][0])[i] = 0;
-    if (ONES)
-        for (int i = threadIdx.x; i < 3 * 64; i += nwaves * 64) (&s_ones[0][0])[i] = 0;
-
-    // ---- the digit rows of this wave's chunks ----
-    const int operand = stage_operand(a.stage_rows), kbytes = a.stage_rows * 16;
-    unsigned char *const my_stage = stage + q0 * TM * 8 * operand;
-    if constexpr (FUSED) {
-        // two vectors at a time (lane 32 v + 2 word + h, as in k_digits), the next two on their way meanwhile
-        const int word = (lane >> 1) & 15, h = lane & 1, vb = lane >> 5;
-        const int pairs = min(TM * VPT / 2, (a.act.batch - n0 + 1) / 2), total = pairs * nq;
-        const int c0 = 512 * q0 + 32 * word + 4 * h;
-        u32x4 v[4], next[4];
-        load_columns(a.act, n0 + vb, c0, 512 * (q0 + 1), v);
-        __builtin_amdgcn_sched_barrier(0);
-        issue(ring[0], ld);
-        __builtin_amdgcn_sched_barrier(0);
-        int i = 0, p = 0;
-#pragma unroll 1
-        for (int k = 0; k < total; ++k) {
-            int i2 = i, p2 = p + 1;
-            if (p2 == pairs) { p2 = 0; ++i2; }
-            if (k + 1 < total) load_columns(a.act, n0 + 2 * p2 + vb, c0 + 512 * i2, 512 * (q0 + i2 + 1), next);
-            convert_columns(a.act, v);
-            u32x4 out[ND];
-            byte_digits<ND>(v, out);
-            const int tm = p / (VPT / 2), g = p % (VPT / 2);
-            unsigned char *dst = my_stage + ((i * TM + tm) * 8 + (word & 3) * 2 + h) * operand + (word >> 2) * kbytes +
-                                 (2 * g + vb) * ND * 16;
-#pragma unroll
-            for (int d = 0; d < ND; ++d) reinterpret_cast<u32x4 *>(dst)[d] = out[d];
-#pragma unroll
-            for (int b = 0; b < 4; ++b) v[b] = next[b];
-            i = i2; p = p2;
-        }
-    } else {
-        issue(ring[0], ld);
-    }
-    if (wave == 0 && lane < PB_MAX_BITS) s_scales[lane] = scv;
-    if (EPI != kSums) {
-        const bool off = lane + 1 < m && !(scv == (lane == 0 ? -2.0f : 2.0f) * scn);
-        merged = __builtin_amdgcn_ballot_w64(off) == 0;
-        if (!merged) {   // the first unit was requested as a whole group
-            ld.e = group_end(0);
-            request_group(ld);
-            issue(ring[0], ld);
-        }
-    }
-    __syncthreads();   // (the sums are zero)
-
-    // prepared digits: lane 16 kb + row of an operand reads the bytes of digit row % ND of vector row / ND
-    // (a top digit that no value needs has no records: the load returns 0 and moves no data)
-    const bool wide = !(PLANES || PLAIN) || is_wide(wide_here);
-    const __amdgpu_buffer_rsrc_t rd = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(a.digits), 0,
-                                                                        (int)a.digits_bytes, 0x00020000);
-    uint32_t doff[TM], dstep[TM];
-    const uint32_t turned = wide && (PLANES || j / 4 == 2) ? 0x80808080u : 0u;
-#pragma unroll
-    for (int tm = 0; tm < TM; ++tm) {
-        const int first = PLANES ? n0 : n0 + tm * VPT, group = first / kGroupVectors, vectors = group_vectors(a.act.batch, group);
-        const int v = first % kGroupVectors + (PLANES ? j : j / (4 * ND) * 4 + j % 4), digit = PLANES ? tm : j / 4 % ND;
-        doff[tm] = v < vectors && (wide || digit < 3) ? digits_at(group, vectors, a.cq, ND, digit, kb, v) : (uint32_t)kNowhere;
-        dstep[tm] = digits_step(vectors, ND);
-    }
-    // staged digits (rows beyond the staged ones belong to no vector: any digits do)
-    const int staged = kb * kbytes + min(j, a.stage_rows - 1) * 16;
-    u32x4 areg[2][TM];
-    auto load_digits = [&](u32x4 (&dst)[TM], int i, int th) {
-#pragma unroll
-        for (int tm = 0; tm < TM; ++tm) {
-            if constexpr (FUSED)
-                dst[tm] = *reinterpret_cast<const u32x4 *>(my_stage + ((i * TM + tm) * 8 + th) * operand + staged);
-            else
-                dst[tm] = __builtin_amdgcn_raw_buffer_load_b128(rd, (int)doff[tm],
-                                                                (int)((uint32_t)((q0 + i) * 8 + th) * dstep[tm]), 0);
-        }
-    };
-
-    Unit u = ld;
-    multiply_group(u);
-    int sets = 0;          // (round, group) pairs multiplied so far
-    int turn = 0;          // the wave that finishes the first tile of a row tile
-    v4i acc[TM], ones;
-    float bias_row = 0.0f, c_old = 0.0f;
-    // the outputs of a row tile: vectors of a lane, tile after tile; the waves take them in turn
-    auto first_item = [&]() { return wave - turn + (wave < turn ? nwaves : 0); };
-    auto vector_of = [&](int item) { return PLANES ? n0 + kb * 4 + item : n0 + item / VPL * VPT + kb * VPL + item % VPL; };
-    const v4i one = {0x01010101, 0x01010101, 0x01010101, 0x01010101};
-    const Masks masks = make_masks();
-    load_digits(areg[0], 0, 0);
-    while (u.r < rounds) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            if (u.r < rounds) {
-                if (advance(ld)) request_group(ld);
-                // (bias and cell state are requested before the next weights: a wait for them does not wait for those)
-                if (a.bias && u.i == nq - 1) bias_row = bias_of(a, (rt0 + u.r) * kTileRows + j);
-                if (EPI == kCell && u.i == nq - 1 && u.e == m) {
-                    const int row = gates_matrix_row((rt0 + u.r) * kTileRows + j, a.gate_h);
-                    c_old = cell_state(a, lane, row, row >= 0, vector_of(first_item()));
-                }
-                issue(ring[k ^ 1], ld);
-                if (u.i == 0) {
-                    ones = v4i{0, 0, 0, 0};
-#pragma unroll
-                    for (int tm = 0; tm < TM; ++tm) acc[tm] = v4i{0, 0, 0, 0};
-                }
-                const uint32_t flip = u.f < 2 ? 0xAAAAAAAAu : 0u;   // (IL) the sign bitlayer is stored complemented
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    uint32_t w[4 * Q];
-                    words_of<Q, IL>(ring[k], t, flip, mask, w);
-                    v4i b[2];
-                    weight_codes<Q, IL, (TM < 4)>(masks, w, b[0], b[1]);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        // the operands of the next step are requested before this step's products
-                        if (t < 3 || h == 0) load_digits(areg[h ^ 1], u.i, t * 2 + h + 1);
-                        else load_digits(areg[0], ld.i, 0);
-                        if constexpr (ONES) ones = __builtin_amdgcn_mfma_i32_16x16x64_i8(one, b[h], ones, 0, 0, 0);
-                        if constexpr (PLANES || PLAIN) areg[h][PLANES ? 2 : 0] ^= turned;   // (a branch here costs more: 16 -> 20 us)
-#pragma unroll
-                        for (int tm = 0; tm < TM; ++tm)
-                            acc[tm] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, areg[h][tm]), b[h],
-                                                                            acc[tm], 0, 0, 0);
-                    }
-                }
-                if (u.i == nq - 1) {
-                    // ---- the group is complete in this wave: the slices of the row meet in LDS ----
-                    // Two buffers of sums, used in turn: the wave that finishes a tile clears its sums, and the buffer is
-                    // added to again only after the next barrier.  The sums of the codes are read by several waves: three
-                    // buffers, each cleared when all have passed the barrier after its reading.
-                    const int buf = sets & 1, buf3 = sets % 3;
-                    if constexpr (ONES) atomicAdd(&s_ones[buf3][lane], ones[0]);
-#pragma unroll
-                    for (int tm = 0; tm < TM; ++tm)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) atomicAdd(&s_sum[buf][tm * 4 + c][lane], acc[tm][c]);
-                    __syncthreads();
-                    ++sets;
-                    if (ONES && wave == 0) s_ones[(buf3 + 2) % 3][lane] = 0;
-                    const Group g = make_group(a, u.f, u.e, s_scales);
-                    const int prow = (rt0 + u.r) * kTileRows + j;
-                    const int row = a.gate_h ? gates_matrix_row(prow, a.gate_h) : prow;
-                    const bool row_ok = row >= 0 && row < a.R;
-                    for (int item = first_item(); item < TM * VPL; item += nwaves) {
-                        const int n = vector_of(item), v = kb * VPL + item % VPL;
-                        int d[ND];
-#pragma unroll
-                        for (int c = 0; c < ND; ++c) {
-                            int *const at = PLANES ? &s_sum[buf][item + 4 * c][lane]
-                                            : FUSED || ND == 1 ? &s_sum[buf][item / VPL * 4 + item % VPL * ND + c][lane]
-                                                    : &s_sum[buf][item / VPL * 4 + v % 4][(v / 4 * ND + c) * 16 + j];
-                            d[c] = *at;
-                            *at = 0;
-                        }
-                        const int sum1 = ONES ? s_ones[buf3][lane] : 0;
-                        if constexpr (EPI == kSums) {
-                            store_sum(a, g, row, row_ok, n, integer_sum<ND>(g, d, sum1, wide));
-                        } else {
-                            double v = scaled_sum<ND>(g, d, sum1, wide);
-                            if (!g.first) v += s_z[item][lane];
-                            if (!g.last) {
-                                s_z[item][lane] = v;
-                            } else {
-                                if (EPI == kCell && item >= nwaves) c_old = cell_state(a, lane, row, row_ok, n);
-                                finish<EPI>(a, lane, row, row_ok, n, v, bias_row, c_old);
-                            }
-                        }
-                    }
-                    if (g.last) {
-                        turn += TM * VPL;
-                        while (turn >= nwaves) turn -= nwaves;
-                    }
-                }
-                if (advance(u)) multiply_group(u);
-            }
-        }
-    }
+// The same product with act(g) u of a gated block behind it.  (One text for both kernels: a function that both call came out with other registers,
+// and with scratch memory in one shape of k_i8.)
+template <int ND, int Q, int TM, bool FUSED>
+__global__ __launch_bounds__(stream_waves(TM) * 64)
+__attribute__((amdgpu_waves_per_eu(stream_waves(TM) / 4, !FUSED && TM == 1 ? 4 : 8))) void k_gated_stream(const I8Args a)
+{
+    constexpr bool IL = false, PLAIN = false;
+    constexpr int EPI = kGated, POLICY = 0;
+#include "pb_i8_stream.inc"
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -414,6 +154,12 @@ static const void *stream_kernel()
 #define PB_I8_ND(ND, E) {{PB_I8_IL(ND, 1, false, E), PB_I8_IL(ND, 1, true, E)}, {PB_I8_IL(ND, 2, false, E), PB_I8_IL(ND, 2, true, E)}}
 #define PB_I8(E) {PB_I8_ND(1, E), PB_I8_ND(2, E), PB_I8_ND(4, E)}
 static const void *const kI8[3][3][2][2][kStreams] = {PB_I8(kStore), PB_I8(kCell), PB_I8(kSums)};
+// (the gated block: [digits][four or eight slots][way])
+#define PB_GATED_Q(ND, Q)                                                                                                          \
+    {reinterpret_cast<const void *>(k_gated_stream<ND, Q, 1, false>), reinterpret_cast<const void *>(k_gated_stream<ND, Q, 4, false>), \
+     reinterpret_cast<const void *>(k_gated_stream<ND, Q, 1, true>), reinterpret_cast<const void *>(k_gated_stream<ND, Q, 2, true>)}
+#define PB_GATED(ND) {PB_GATED_Q(ND, 1), PB_GATED_Q(ND, 2)}
+static const void *const kGatedFn[3][2][4] = {PB_GATED(1), PB_GATED(2), PB_GATED(4)};
 
 // Staged digits of a workgroup at most (a compute unit has 160 KB of LDS)
 constexpr int kMaxStage = 140 * 1024;
@@ -568,7 +314,7 @@ int launch_imma(const uint32_t *packed, const float *scales, const Layout &L, in
     a.wide = static_cast<const uint8_t *>(wide);
     a.act = act_source(X0, cols0, X1, cols1, batch, frac_bits, act_bits);
     a.scales = scales; a.Y = Y; a.A = A; a.pairs_out = (A && pairs_out) ? 1 : 0;
-    a.bias = ep.bias; a.relu = ep.relu; a.c_prev = ep.c_prev; a.h_out = ep.h_out; a.c_out = ep.c_out;
+    a.bias = ep.bias; a.relu = ep.relu; a.c_prev = ep.c_prev; a.h_out = ep.h_out; a.c_out = ep.c_out; a.gate = ep.gate;
     a.gate_h = L.gate_h; a.R = L.rows;
     a.out_scale = ldexp(1.0, -frac_bits);
     // (the epilogue addresses the bias and the cell state with 32-bit byte offsets)
@@ -585,27 +331,33 @@ int launch_imma(const uint32_t *packed, const float *scales, const Layout &L, in
     const hipError_t no_device = compute_units(&cus);
     if (no_device != hipSuccess) return (int)no_device;
     int way = pick_way(c, prepared, cus);
-    if (way == kFusedNt && (A || ep.c_prev)) way = kFused1;
+    if (way == kFusedNt && (A || ep.fused())) way = kFused1;
     // Third digits as they stand: what pb_act_prep leaves; and with at most four bitlayers and more than four tiles, whose digits take longer to read
     // than flags and XOR (1291 x 9493, 4 bitlayers, 17 vectors 11.5 us, all four digits 12.4; 393 x 14185, 2 bitlayers, 29 vectors 9.5, 9.9;
     // but 16337 x 1799, 4 bitlayers, 3 vectors 6.9, 6.5, and 870 x 9440, 8 bitlayers, 21 vectors 13.5, 12.5).
-    if (way == kMemory1 && nd == 4 && (prepared || (c.tiles > 4 && bits_used <= 4 && !A && !ep.c_prev))) way = kPlain1;
+    if (way == kMemory1 && nd == 4 && (prepared || (c.tiles > 4 && bits_used <= 4 && !A && !ep.fused()))) way = kPlain1;
     const int shape = way - kStreams;
     if (!prepared && !is_fused(way)) {
         const int e = launch_digits(X0, cols0, X1, cols1, batch, L, frac_bits, act_bits, digits, wide, nullptr, way != kMemory1, st);
         if (e) return e;
     }
-    if (shape >= 0) return launch_imma_tile(shape, a, nd, il, st);
+    if (shape >= 0) {
+        if (a.gate < 0) return launch_imma_tile(shape, a, nd, il, st);
+        // a gated block: the pre-activations through memory
+        if (!a.Y) a.Y = ep.pre;
+        const int e = launch_imma_tile(shape, a, nd, il, st);
+        return e ? e : launch_gated(a.Y, L.rows / 2, ep.gate, batch, ep.h_out, st);
+    }
 
-    const int epi = A ? kSums : (ep.c_prev ? kCell : kStore), q = (!A && bits_used > 4) ? 1 : 0;
+    const int epi = A ? kSums : (ep.c_prev ? kCell : (ep.gate >= 0 ? kGated : kStore)), q = (!A && bits_used > 4) ? 1 : 0;
     const int ndi = nd == 4 ? 2 : nd - 1, tm = way_tiles(way);
-    const void *fn = kI8[epi][ndi][q][il][way];
+    const void *fn = epi == kGated ? kGatedFn[ndi][q][way] : kI8[epi][ndi][q][il][way];
     if (!fn) return (int)hipErrorInvalidValue;
     a.chunks_per_wave = slice(L.cq, tm);
     a.stage_rows = stage_rows(c, tm);
     const int S = (L.cq + a.chunks_per_wave - 1) / a.chunks_per_wave;
     const size_t lds = is_fused(way) ? stage_bytes(c, tm) : 0;
-    static int cache[3][3][2][2][kStreams][17][24];   // (the last index: LDS in steps of 6 KB)
+    static int cache[4][3][2][2][kStreams][17][24];   // (the last index: LDS in steps of 6 KB)
     int most = per_unit(fn, S * 64, (size_t)stream_lds(nd, tm, epi), lds, &cache[epi][ndi][q][il][way][S][lds / 6144]);
     if (most < 1) return (int)hipErrorInvalidValue;
     if (is_fused(way) && most > fused_per_cu(S)) most = fused_per_cu(S);

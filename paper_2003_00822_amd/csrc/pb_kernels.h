@@ -27,12 +27,16 @@ int launch_matvec(const uint32_t *packed, const float *scales, const Layout &L, 
 // the pairs layout).  Activations come from X0 / X1 (converted and bit-transposed inside the kernel) or, if `planes` is
 // non-null, from bit planes that launch_prep left in memory.  Exactly one of Y / A is non-null.
 // What follows the product in the same launch: bias and ReLU before the store of Y, or (PB_LAYOUT_TILE16_GATES_V1
-// only) the LSTM cell update, which writes h_out / c_out [batch][H] instead of Y.
+// only) the LSTM cell update, which writes h_out / c_out [batch][H] instead of Y, or a gated block's act(g) u, which writes
+// h_out [batch][rows / 2] and, where wanted, the pre-activations to Y.
 struct Epilogue {
     const float *bias = nullptr;   // [rows] or null
     int relu = 0;
     const float *c_prev = nullptr; // non-null: fused LSTM cell
     float *h_out = nullptr, *c_out = nullptr;
+    int gate = -1;                 // 0 or more: fused gated block (a pb_gate)
+    float *pre = nullptr;          // room for its pre-activations, which go through memory where there are many vectors
+    bool fused() const { return c_prev || gate >= 0; }
 };
 int launch_mfma(const uint32_t *packed, const float *scales, const Layout &L, int bits_used, int frac_bits,
                 int act_bits, const float *X0, int cols0, const float *X1, int cols1, const uint32_t *planes, float *Y,

@@ -82,6 +82,7 @@ struct MfmaArgs {
     float fscale;               // 2^frac_bits
     int imin, imax;             // range of the act_bits-bit fixed-point values
     double out_scale;           // 2^-frac_bits
+    int gate;                   // (GATED) act(g) u of a gated block goes to h_out, the pre-activations to Y if that is non-null
 };
 
 // z + (z of the lane D lanes away, D = 16 or 32), in both lanes
@@ -184,7 +185,7 @@ __device__ __forceinline__ v4f mfma_fp4(const v8i a, const v8i b, const v4f c)
 // the registers a wave may use; RU: units (row tile, bitlayer) whose blocks a wave has in flight.  The host picks
 // RU <= the units a wave has, so that a short stream pays for no empty ring slots; 4 KB in flight per wave
 // measured best (more requests in flight than that slow the short streams down and do not speed up the long ones).
-template <int NQ, int MAXS, int RU>
+template <int NQ, int MAXS, int RU, bool GATED = false>
 __global__ __launch_bounds__(MAXS * 64) void k_mfma(const uint32_t *packed, const float *X0, uint32_t packed_bytes,
                                                     uint32_t flags, int cols0, uint32_t layer_step,
                                                     uint32_t round_step, int rounds_per_wg, int rt_count, int cq,
@@ -494,6 +495,13 @@ __global__ __launch_bounds__(MAXS * 64) void k_mfma(const uint32_t *packed, cons
                                     a.c_out[row] = cn;
                                     a.h_out[row] = hn;
                                 }
+                            } else if (GATED) {
+                                // the first two lanes of a quad hold the gates of two units, the others their values
+                                const float hn = gated_quad(a.gate, y);
+                                if (row_ok && lg == 0) {
+                                    if (a.Y) a.Y[row] = y;
+                                    if ((lane & 2) == 0) a.h_out[row] = hn;
+                                }
                             } else {
                                 if (a.relu) y = fmaxf(y, 0.0f);
                                 if (row_ok && lg == 0) a.Y[row] = y;
@@ -513,8 +521,10 @@ __global__ __launch_bounds__(MAXS * 64) void k_mfma(const uint32_t *packed, cons
 struct Variant {
     int nq, maxs, ru;
     const void *fn;
+    const void *gated;     // with act(g) u of a gated block behind the product
 };
-#define PB_VARIANT(NQ, MAXS, RU) {NQ, MAXS, RU, reinterpret_cast<const void *>(k_mfma<NQ, MAXS, RU>)}
+#define PB_VARIANT(NQ, MAXS, RU) \
+    {NQ, MAXS, RU, reinterpret_cast<const void *>(k_mfma<NQ, MAXS, RU>), reinterpret_cast<const void *>(k_mfma<NQ, MAXS, RU, true>)}
 static const Variant kVariants[] = {
     PB_VARIANT(1, 16, 1), PB_VARIANT(1, 16, 2), PB_VARIANT(1, 16, 4),
     PB_VARIANT(2, 16, 1), PB_VARIANT(2, 16, 2), PB_VARIANT(2, 16, 3),
@@ -591,8 +601,8 @@ static int resident_workgroups(int variant, int S)
         for (int i = 0; i < kNumVariants; ++i) {
             const Variant &o = kVariants[i];
             if (o.nq != kVariants[variant].nq || o.maxs != kVariants[variant].maxs) continue;
-            if (hipFuncSetAttribute(o.fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)stage_bytes(S)) != hipSuccess)
-                return 0;
+            for (const void *fn : {o.fn, o.gated})
+                if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)stage_bytes(S)) != hipSuccess) return 0;
         }
     }
     if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kVariants[variant].fn, S * 64, stage_bytes(S)) != hipSuccess)
@@ -609,7 +619,7 @@ int launch_mfma(const uint32_t *packed, const float *scales, const Layout &L, in
     MfmaArgs a;
     MfmaHead h;
     h.packed = packed; h.X0 = X0; a.X1 = X1; a.planes = planes; a.scales = scales; a.Y = Y; a.A = A;
-    a.bias = ep.bias; a.relu = ep.relu; a.c_prev = ep.c_prev; a.h_out = ep.h_out; a.c_out = ep.c_out;
+    a.bias = ep.bias; a.relu = ep.relu; a.c_prev = ep.c_prev; a.h_out = ep.h_out; a.c_out = ep.c_out; a.gate = ep.gate;
     a.gate_h = L.gate_h;
     // (the epilogue addresses the bias and the cell state with 32-bit byte offsets)
     if (ep.bias && L.rows >= (1 << 29)) return (int)hipErrorInvalidValue;
@@ -640,7 +650,7 @@ int launch_mfma(const uint32_t *packed, const float *scales, const Layout &L, in
     const Variant &run = kVariants[pick_ring(vi, h.rounds_per_wg * bits_used)];
     void *args[] = {&h.packed, &h.X0, &h.packed_bytes, &h.flags, &h.cols0, &h.layer_step, &h.round_step,
                     &h.rounds_per_wg, &h.rt_count, &h.cq, &h.m, &a};
-    const hipError_t e = hipLaunchKernel(run.fn, dim3((unsigned)wgs), dim3((unsigned)S * 64), args,
+    const hipError_t e = hipLaunchKernel(ep.gate >= 0 ? run.gated : run.fn, dim3((unsigned)wgs), dim3((unsigned)S * 64), args,
                                          planes ? 0 : stage_bytes(S), st);
     return (int)(e != hipSuccess ? e : hipGetLastError());
 }
