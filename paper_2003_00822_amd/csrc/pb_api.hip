@@ -473,6 +473,7 @@ int pb_matmul_adapters(const void *packed, const float *scales, const pb_desc *d
     if (err) return hip_status(err);
     pb::Epilogue ep;
     ep.bias = bias;
+    ep.pre = reinterpret_cast<float *>(static_cast<char *>(workspace) + pb::ws_gates_off(L, batch));
     rc = matmul_common(packed, scales, d, bits_used, X, d->cols, nullptr, 0, batch, Y, nullptr, workspace, stream, ep, false, true);
     if (rc != PB_OK) return rc;
     return hip_status(pb::launch_adapter_up(p, *adapters, L, index, batch, Y, ws, st));

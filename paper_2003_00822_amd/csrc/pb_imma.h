@@ -386,4 +386,9 @@ inline int tile_rows(const TileShape &t, int m, bool sums)
 }
 int launch_imma_tile(int shape, const I8Args &a, int nd, bool il, hipStream_t st);
 
+// The kernel for large batches of the gated block and the adapters (pb_batch.hip): its workgroups, its launch (`partial`: [batch][R], used where
+// there are several groups of bitlayers)
+int batch_workgroups(int rt_count, int batch);
+int launch_imma_batch(const I8Args &a, bool il, float *partial, hipStream_t st);
+
 }  // namespace pb

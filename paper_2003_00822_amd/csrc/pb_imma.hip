@@ -330,6 +330,11 @@ int launch_imma(const uint32_t *packed, const float *scales, const Layout &L, in
     int cus;
     const hipError_t no_device = compute_units(&cus);
     if (no_device != hipSuccess) return (int)no_device;
+    // Large batches of the operators: the kernel of pb_batch.hip where it fills three quarters of the chip
+    if (ep.pre && nd == 4 && batch > 64 && batch_workgroups(L.rt_count, batch) >= cus * 3 / 4) {
+        const int e = launch_digits(X0, cols0, X1, cols1, batch, L, frac_bits, act_bits, digits, wide, nullptr, true, st);
+        return e ? e : launch_imma_batch(a, il, ep.pre, st);
+    }
     int way = pick_way(c, prepared, cus);
     if (way == kFusedNt && (A || ep.fused())) way = kFused1;
     // Third digits as they stand: what pb_act_prep leaves; and with at most four bitlayers and more than four tiles, whose digits take longer to read

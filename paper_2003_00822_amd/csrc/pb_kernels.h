@@ -35,7 +35,7 @@ struct Epilogue {
     const float *c_prev = nullptr; // non-null: fused LSTM cell
     float *h_out = nullptr, *c_out = nullptr;
     int gate = -1;                 // 0 or more: fused gated block (a pb_gate)
-    float *pre = nullptr;          // room for its pre-activations, which go through memory where there are many vectors
+    float *pre = nullptr;          // non-null: room for [batch][rows], and the kernel for large batches of pb_batch.hip may be taken
     bool fused() const { return c_prev || gate >= 0; }
 };
 int launch_mfma(const uint32_t *packed, const float *scales, const Layout &L, int bits_used, int frac_bits,

@@ -259,6 +259,47 @@ def test_gated_block(pb, units, cols, bits, m, batch, layout):
             assert torch.equal(alone, H)
 
 
+LARGE = [  # rows, cols, bits, used, batch, layout, scales that do not halve: at least 192 workgroups of 128 rows and 128 vectors
+    (3100, 515, 8, 8, 1000, "gates", False), (3096, 1100, 5, 4, 1001, "gates", False), (6200, 64, 2, 1, 500, "gates", False),
+    (3100, 520, 12, 11, 1000, "gates", False), (3100, 300, 6, 6, 950, "gates", True), (3100, 515, 8, 8, 1000, "bits", False),
+    (3090, 1100, 8, 7, 1021, "pairs", False), (6200, 33, 4, 4, 520, "pairs", False), (3100, 520, 16, 16, 1000, "pairs", False),
+    (3100, 300, 3, 3, 990, "bits", True), (24600, 40, 8, 8, 65, "bits", False),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols,bits,m,batch,layout,odd_scales", LARGE)
+def test_large_batches(pb, rows, cols, bits, m, batch, layout, odd_scales):
+    """Values of three digits, and in some groups of sixteen vectors of four; a gated block, or a layer with adapters."""
+    scales = np.array([-1.5, 0.7, 0.01, 3.0, -0.2, 1.0][:bits], dtype=np.float32) * 0.1 if odd_scales else None
+    layer = Layer(pb, rows, cols, bits, LAYOUTS[layout], scales=scales)
+    g = np.random.default_rng(12)
+    X = g.standard_normal((batch, cols)).astype(np.float32)
+    X[[3, batch // 2, batch - 1]] *= 300
+    X[5, cols - 1], X[40, 0] = 1e9, -1e9                    # beyond the range of the fixed point
+    bias = g.standard_normal(rows).astype(np.float32)
+    W, Xd, bd = layer.matrix(m), torch.from_numpy(X).cuda(), torch.from_numpy(bias).cuda()
+    product = fixed(X) @ W.T
+    terms = sum(abs(float(layer.scales[i])) * layer.layers[i].reshape(rows, cols) for i in range(m)) if odd_scales else np.abs(W)
+    # one rounding per group of bitlayers (at most three, or each bitlayer by itself) and its sum, one of the sum with the bias
+    groups = m if odd_scales else 1 + (m > 8) + (m > 14)
+    tol = U * (np.abs(product + bias) + 2 * groups * (np.abs(fixed(X)) @ terms.T if groups > 1 else np.abs(product))) + 1e-12 * (np.abs(fixed(X)) @ terms.T)
+    if layout == "gates":
+        units = rows // 2
+        H, pre = layer.lin.gated(Xd, 1, m, bias=bd, keep=True)
+        close(pre, product + bias, tol, "pre")
+        p = pre.cpu().numpy().astype(np.float64)
+        a, da = gate_of(1, p[:, :units])
+        # (exp overflows at 2^128: a logistic function below 2^-128 is 0, as a factor of v u)
+        tol = 16 * U * np.abs(a * p[:, units:]) + 8 * U * np.abs(p[:, :units] * da * p[:, units:]) + 2.0 ** -127 * np.abs(p[:, :units] * p[:, units:])
+        close(H, a * p[:, units:], tol + 1e-40, "H")
+        assert torch.equal(layer.lin.gated(Xd, 1, m, bias=bd), H)
+    else:
+        zero = pb.Adapters(torch.zeros((1, 1, cols), device="cuda"), torch.zeros((1, rows, 1), device="cuda"))
+        Y = layer.lin.adapted(Xd, zero, torch.full((batch,), -1, dtype=torch.int32, device="cuda"), m, bias=bd)
+        close(Y, product + bias, tol, "Y")
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("gate", [0, 1, 2, 3])
 def test_gates_far_out(pb, gate):
