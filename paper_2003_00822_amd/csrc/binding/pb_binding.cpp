@@ -11,6 +11,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 
@@ -39,6 +40,13 @@ const char *const kNames[kEntries] = {
 void *g_fn[kEntries];               // null until bound: every call then goes to `slow`
 PyObject *g_slow[kEntries];
 PyObject *g_slow_linear = nullptr;
+// PackedLinear's operators, and the sizes of their workspaces
+enum Method { kGated, kGatedGrad, kGrad, kAdapted, kAdaptedGrad, kOperators };
+const char *const kMethodNames[kOperators] = {"gated", "gated_grad", "grad", "adapted", "adapted_grad"};
+PyObject *g_slow_method[kOperators];
+decltype(&pb_workspace_bytes) g_workspace_bytes;
+decltype(&pb_grad_workspace_bytes) g_grad_workspace_bytes;
+decltype(&pb_adapters_workspace_bytes) g_adapters_workspace_bytes;
 
 // ---- arguments: `load` says whether the object is what the fast path expects ----
 template <typename T, at::ScalarType DT, bool NULLABLE = false>
@@ -155,11 +163,12 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kw
 }
 
 PyObject *s_rows, *s_cols, *s_bits, *s_max_batch, *s_desc, *s_packed, *s_scales, *s_workspace, *s_home_stream;
+PyObject *s_count, *s_rank, *s_A, *s_B, *s_scale;
 
 // The attributes of `self` that a call uses, held until it returns: one that is computed on access, or replaced by another
 // thread meanwhile, must not give its memory back before the launch.
 struct Held {
-    PyObject *o[9];
+    PyObject *o[16];
     int n = 0;
     int workspace = 0;   // which of them
     ~Held() { while (n) Py_DECREF(o[--n]); }
@@ -232,6 +241,243 @@ PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     return PyObject_Vectorcall(g_slow_linear, args, nargs, nullptr);
 }
 
+// ---- PackedLinear's operators: f(self, every argument), with outputs and a workspace made here.  What is not as they expect it goes to the Python
+// functions in pb.py, as above. ----
+const at::Tensor *tensor(PyObject *o) { return THPVariable_CheckExact(o) ? &THPVariable_Unpack(o) : nullptr; }
+bool plain(const at::Tensor *t, const at::Device &device, at::ScalarType type)
+{
+    return t && t->is_cuda() && t->scalar_type() == type && t->is_contiguous() && t->device() == device;
+}
+
+// What every operator uses of the layer
+struct Layer {
+    Held held;
+    Int rows, cols, m;
+    Desc d;
+    Bytes packed;
+    In scales;
+    at::Device device = at::kCPU;
+    bool load(PyObject *self, PyObject *bits_used)
+    {
+        if (!g_workspace_bytes || !held.load(self, s_packed, packed)) return false;
+        device = THPVariable_Unpack(held.o[held.n - 1]).device();
+        return device.index() == c10::hip::current_device() && held.load(self, s_rows, rows) && held.load(self, s_cols, cols) &&
+               held.load(self, s_desc, d) && held.load(self, s_scales, scales) &&
+               (bits_used == Py_None ? held.load(self, s_bits, m) : m.load(bits_used));
+    }
+    // n vectors of `length` values
+    const float *vectors(PyObject *o, int length, int64_t *n) const
+    {
+        const at::Tensor *t = tensor(o);
+        if (!plain(t, device, at::kFloat) || t->dim() != 2 || t->size(1) != length || t->size(0) < 1 || t->size(0) > PB_MAX_BATCH) return nullptr;
+        if (*n && *n != t->size(0)) return nullptr;
+        *n = t->size(0);
+        return static_cast<const float *>(t->data_ptr());
+    }
+    // `length` values or None
+    template <typename T>
+    bool values(PyObject *o, at::ScalarType type, int64_t length, const T **p) const
+    {
+        *p = nullptr;
+        if (o == Py_None) return true;
+        const at::Tensor *t = tensor(o);
+        if (!plain(t, device, type) || t->dim() != 1 || t->size(0) != length) return false;
+        *p = static_cast<const T *>(t->data_ptr());
+        return true;
+    }
+    at::Tensor floats(at::IntArrayRef shape) const { return at::empty(shape, at::TensorOptions().dtype(at::kFloat).device(device)); }
+    at::Tensor work(size_t bytes) const
+    {
+        return at::empty({(int64_t)(bytes > 16 ? bytes : 16)}, at::TensorOptions().dtype(at::kByte).device(device));
+    }
+};
+float *floats_of(const at::Tensor &t) { return static_cast<float *>(t.data_ptr()); }
+
+// The tensors of an Adapters object as they are now, held until the call returns
+struct AdapterSet {
+    Held held;
+    pb_adapters v{};
+    at::Tensor A, B;
+    bool load(PyObject *o, const Layer &l)
+    {
+        Int count, rank, rows, cols;
+        PyObject *a = PyObject_GetAttr(o, s_A), *b = a ? PyObject_GetAttr(o, s_B) : nullptr, *s = b ? PyObject_GetAttr(o, s_scale) : nullptr;
+        for (PyObject *x : {a, b, s})
+            if (x) held.o[held.n++] = x;
+        if (!s) { PyErr_Clear(); return false; }
+        if (!held.load(o, s_count, count) || !held.load(o, s_rank, rank) || !held.load(o, s_rows, rows) || !held.load(o, s_cols, cols)) return false;
+        const at::Tensor *ta = tensor(a), *tb = tensor(b);
+        if (!ta || !tb || rows.v != l.rows.v || cols.v != l.cols.v) return false;
+        const at::ScalarType type = ta->scalar_type();
+        if (type != at::kFloat && type != at::kBFloat16 && type != at::kHalf) return false;
+        if (!plain(ta, l.device, type) || !plain(tb, l.device, type)) return false;
+        if (ta->sizes() != at::IntArrayRef({count.v, rank.v, cols.v}) || tb->sizes() != at::IntArrayRef({count.v, rows.v, rank.v})) return false;
+        if (!l.values(s, at::kFloat, count.v, &v.scale)) return false;
+        A = *ta;
+        B = *tb;
+        v.count = count.v;
+        v.rank = rank.v;
+        v.type = type == at::kFloat ? PB_TYPE_F32 : (type == at::kBFloat16 ? PB_TYPE_BF16 : PB_TYPE_F16);
+        v.A = ta->data_ptr();
+        v.B = tb->data_ptr();
+        return true;
+    }
+};
+
+template <typename F>
+int without_gil(F f)
+{
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f();
+    Py_END_ALLOW_THREADS
+    return rc;
+}
+template <typename... T>
+PyObject *tuple_of(T... tensors)      // an undefined tensor is None
+{
+    PyObject *t = PyTuple_New(sizeof...(T));
+    if (!t) return nullptr;
+    Py_ssize_t i = 0;
+    auto put = [&](at::Tensor &x) {
+        PyObject *o = x.defined() ? THPVariable_Wrap(std::move(x)) : Py_NewRef(Py_None);
+        if (!o) return false;
+        PyTuple_SET_ITEM(t, i++, o);
+        return true;
+    };
+    if (!(put(tensors) && ...)) {
+        Py_DECREF(t);
+        return nullptr;
+    }
+    return t;
+}
+// f(args) sets *result (or an error) where it takes the call
+template <Method M, int N, typename F>
+PyObject *method(PyObject *const *args, Py_ssize_t nargs, F f)
+{
+    if (nargs == N) {
+        try {
+            PyObject *result = nullptr;
+            if (f(args, &result)) return result;
+        } catch (const std::exception &) {
+        }
+        if (PyErr_Occurred()) PyErr_Clear();
+    }
+    return PyObject_Vectorcall(g_slow_method[M], args, nargs, nullptr);
+}
+
+// gated(self, X, gate, bits_used, bias, keep)
+PyObject *gated(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    return method<kGated, 6>(args, nargs, [](PyObject *const *a, PyObject **result) {
+        Layer l;
+        Int gate;
+        int64_t n = 0;
+        const float *x, *bias;
+        if (!l.load(a[0], a[3]) || !(x = l.vectors(a[1], l.cols.v, &n)) || !gate.load(a[2]) || !l.values(a[4], at::kFloat, l.rows.v, &bias)) return false;
+        if (a[5] != Py_True && a[5] != Py_False) return false;
+        at::Tensor H = l.floats({n, l.rows.v / 2}), pre = a[5] == Py_True ? l.floats({n, l.rows.v}) : at::Tensor();
+        const at::Tensor work = l.work(g_workspace_bytes(&l.d.v, (int)n));
+        void *stream = current_stream();
+        const int rc = without_gil([&] {
+            return reinterpret_cast<decltype(&pb_gated_linear)>(g_fn[kGatedLinear])(l.packed.v, l.scales.v, &l.d.v, l.m.v, x, (int)n, bias, gate.v, floats_of(H),
+                                                                                    pre.defined() ? floats_of(pre) : nullptr, work.data_ptr(), stream);
+        });
+        if (rc != PB_OK) *result = status_result(rc, kNames[kGatedLinear]);
+        else *result = pre.defined() ? tuple_of(H, pre) : THPVariable_Wrap(std::move(H));
+        return true;
+    });
+}
+
+// gated_grad(self, pre, dH, gate, bits_used)
+PyObject *gated_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    return method<kGatedGrad, 5>(args, nargs, [](PyObject *const *a, PyObject **result) {
+        Layer l;
+        Int gate;
+        int64_t n = 0;
+        const float *pre, *dH;
+        if (!l.load(a[0], a[4]) || !(pre = l.vectors(a[1], l.rows.v, &n)) || !(dH = l.vectors(a[2], l.rows.v / 2, &n)) || !gate.load(a[3])) return false;
+        at::Tensor dX = l.floats({n, l.cols.v}), dpre = l.floats({n, l.rows.v});
+        const at::Tensor work = l.work(g_grad_workspace_bytes(&l.d.v, (int)n));
+        void *stream = current_stream();
+        const int rc = without_gil([&] {
+            return reinterpret_cast<decltype(&pb_gated_linear_grad)>(g_fn[kGatedLinearGrad])(l.packed.v, l.scales.v, &l.d.v, l.m.v, pre, dH, (int)n, gate.v,
+                                                                                             floats_of(dpre), floats_of(dX), work.data_ptr(), stream);
+        });
+        *result = rc != PB_OK ? status_result(rc, kNames[kGatedLinearGrad]) : tuple_of(dX, dpre);
+        return true;
+    });
+}
+
+// grad(self, dY, bits_used)
+PyObject *grad(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    return method<kGrad, 3>(args, nargs, [](PyObject *const *a, PyObject **result) {
+        Layer l;
+        int64_t n = 0;
+        const float *dY;
+        if (!l.load(a[0], a[2]) || !(dY = l.vectors(a[1], l.rows.v, &n))) return false;
+        at::Tensor dX = l.floats({n, l.cols.v});
+        const at::Tensor work = l.work(g_grad_workspace_bytes(&l.d.v, (int)n));
+        void *stream = current_stream();
+        const int rc = without_gil([&] {
+            return reinterpret_cast<decltype(&pb_matmul_grad)>(g_fn[kMatmulGrad])(l.packed.v, l.scales.v, &l.d.v, l.m.v, dY, (int)n, floats_of(dX),
+                                                                                  work.data_ptr(), stream);
+        });
+        *result = rc != PB_OK ? status_result(rc, kNames[kMatmulGrad]) : THPVariable_Wrap(std::move(dX));
+        return true;
+    });
+}
+
+// adapted(self, X, adapters, index, bits_used, bias)
+PyObject *adapted(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    return method<kAdapted, 6>(args, nargs, [](PyObject *const *a, PyObject **result) {
+        Layer l;
+        AdapterSet set;
+        int64_t n = 0;
+        const float *x, *bias;
+        const int32_t *index;
+        if (!l.load(a[0], a[4]) || !(x = l.vectors(a[1], l.cols.v, &n)) || !l.values(a[3], at::kInt, n, &index) ||
+            !l.values(a[5], at::kFloat, l.rows.v, &bias) || !set.load(a[2], l)) return false;
+        at::Tensor Y = l.floats({n, l.rows.v});
+        const at::Tensor work = l.work(g_adapters_workspace_bytes(&l.d.v, &set.v, (int)n));
+        void *stream = current_stream();
+        const int rc = without_gil([&] {
+            return reinterpret_cast<decltype(&pb_matmul_adapters)>(g_fn[kMatmulAdapters])(l.packed.v, l.scales.v, &l.d.v, l.m.v, x, (int)n, &set.v, index, bias,
+                                                                                          floats_of(Y), work.data_ptr(), stream);
+        });
+        *result = rc != PB_OK ? status_result(rc, kNames[kMatmulAdapters]) : THPVariable_Wrap(std::move(Y));
+        return true;
+    });
+}
+
+// adapted_grad(self, X, dY, adapters, index, bits_used, inputs)
+PyObject *adapted_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    return method<kAdaptedGrad, 7>(args, nargs, [](PyObject *const *a, PyObject **result) {
+        Layer l;
+        AdapterSet set;
+        int64_t n = 0;
+        const float *x, *dY;
+        const int32_t *index;
+        if (!l.load(a[0], a[5]) || !(x = l.vectors(a[1], l.cols.v, &n)) || !(dY = l.vectors(a[2], l.rows.v, &n)) ||
+            !l.values(a[4], at::kInt, n, &index) || !set.load(a[3], l)) return false;
+        if (a[6] != Py_True && a[6] != Py_False) return false;
+        at::Tensor dX = a[6] == Py_True ? l.floats({n, l.cols.v}) : at::Tensor(), dA = l.floats(set.A.sizes()), dB = l.floats(set.B.sizes());
+        const at::Tensor work = l.work(g_adapters_workspace_bytes(&l.d.v, &set.v, (int)n));
+        void *stream = current_stream();
+        const int rc = without_gil([&] {
+            return reinterpret_cast<decltype(&pb_matmul_adapters_grad)>(g_fn[kMatmulAdaptersGrad])(
+                l.packed.v, l.scales.v, &l.d.v, l.m.v, x, dY, (int)n, &set.v, index, dX.defined() ? floats_of(dX) : nullptr, floats_of(dA), floats_of(dB),
+                work.data_ptr(), stream);
+        });
+        *result = rc != PB_OK ? status_result(rc, kNames[kMatmulAdaptersGrad]) : tuple_of(dX, dA, dB);
+        return true;
+    });
+}
+
 // bind(desc_type, adapters_type, error_type, {name: address})
 PyObject *bind(PyObject *, PyObject *args)
 {
@@ -244,6 +490,14 @@ PyObject *bind(PyObject *, PyObject *args)
         p[e] = PyLong_AsVoidPtr(a);
         if (!p[e]) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "%s", kNames[e]);
     }
+    void *sizes[3];
+    const char *const size_names[3] = {"pb_workspace_bytes", "pb_grad_workspace_bytes", "pb_adapters_workspace_bytes"};
+    for (int i = 0; i < 3; ++i) {
+        PyObject *a = PyDict_GetItemString(fns, size_names[i]);
+        if (!a) return PyErr_Format(PyExc_KeyError, "%s", size_names[i]);
+        sizes[i] = PyLong_AsVoidPtr(a);
+        if (!sizes[i]) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "%s", size_names[i]);
+    }
     Py_INCREF(desc);
     Py_INCREF(adapters);
     Py_INCREF(error);
@@ -254,17 +508,21 @@ PyObject *bind(PyObject *, PyObject *args)
     g_adapters_type = adapters;
     g_error = error;
     for (int e = 0; e < kEntries; ++e) g_fn[e] = p[e];
+    g_grad_workspace_bytes = reinterpret_cast<decltype(&pb_grad_workspace_bytes)>(sizes[1]);
+    g_adapters_workspace_bytes = reinterpret_cast<decltype(&pb_adapters_workspace_bytes)>(sizes[2]);
+    g_workspace_bytes = reinterpret_cast<decltype(&pb_workspace_bytes)>(sizes[0]);
     Py_RETURN_NONE;
 }
 
-// set_slow({name: function}): the Python functions behind the fast ones ("linear" for PackedLinear.__call__)
+// set_slow({name: function}): the Python functions behind the fast ones ("linear" for PackedLinear.__call__, "gated" for PackedLinear.gated, ...)
 PyObject *set_slow(PyObject *, PyObject *fns)
 {
     if (!PyDict_Check(fns)) return PyErr_Format(PyExc_TypeError, "a dict of functions");
-    for (int e = 0; e <= kEntries; ++e) {
-        PyObject *f = PyDict_GetItemString(fns, e < kEntries ? kNames[e] : "linear");
-        if (!f) return PyErr_Format(PyExc_KeyError, "%s", e < kEntries ? kNames[e] : "linear");
-        PyObject **slot = e < kEntries ? &g_slow[e] : &g_slow_linear;
+    for (int e = 0; e <= kEntries + kOperators; ++e) {
+        const char *name = e < kEntries ? kNames[e] : (e == kEntries ? "linear" : kMethodNames[e - kEntries - 1]);
+        PyObject *f = PyDict_GetItemString(fns, name);
+        if (!f) return PyErr_Format(PyExc_KeyError, "%s", name);
+        PyObject **slot = e < kEntries ? &g_slow[e] : (e == kEntries ? &g_slow_linear : &g_slow_method[e - kEntries - 1]);
         Py_INCREF(f);
         Py_XDECREF(*slot);
         *slot = f;
@@ -314,6 +572,11 @@ PyMethodDef kMethods[] = {
     fast<&pb_matmul_adapters_grad, kMatmulAdaptersGrad, Bytes, In, Desc, Int, In, In, Int, Adapters, IntsOrNone, OutOrNone, OutOrNone,
          OutOrNone, Bytes>(),
     {"linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&linear)), METH_FASTCALL, nullptr},
+    {"gated", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&gated)), METH_FASTCALL, nullptr},
+    {"gated_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&gated_grad)), METH_FASTCALL, nullptr},
+    {"grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&grad)), METH_FASTCALL, nullptr},
+    {"adapted", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&adapted)), METH_FASTCALL, nullptr},
+    {"adapted_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&adapted_grad)), METH_FASTCALL, nullptr},
     {"bind", bind, METH_VARARGS, nullptr},
     {"set_slow", set_slow, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
@@ -334,6 +597,11 @@ PyMODINIT_FUNC PyInit__binding()
     s_scales = PyUnicode_InternFromString("scales");
     s_workspace = PyUnicode_InternFromString("workspace");
     s_home_stream = PyUnicode_InternFromString("home_stream");
+    s_count = PyUnicode_InternFromString("count");
+    s_rank = PyUnicode_InternFromString("rank");
+    s_A = PyUnicode_InternFromString("A");
+    s_B = PyUnicode_InternFromString("B");
+    s_scale = PyUnicode_InternFromString("scale");
     PyObject *m = PyModule_Create(&kModule);
     if (m && PyModule_AddStringConstant(m, "BUILT_FOR", PB_BUILT_FOR) != 0) Py_CLEAR(m);   // (pb.py compares it)
     return m;

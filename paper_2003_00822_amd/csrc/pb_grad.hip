@@ -38,51 +38,57 @@ __device__ __forceinline__ Scaling scaling_of(uint32_t largest, double squares, 
     return {30 - e, 23 - e - (f * 8388608.0f > 8355000.0f ? 1 : 0), most * most * count > 144.0 * squares ? 1 : 0, 0};
 }
 
-// The largest of a value per thread and the sum of another, in thread 0
-template <int WAVES>
-__device__ __forceinline__ void over_workgroup(uint32_t &most, double &sum)
-{
-    __shared__ uint32_t s_max[WAVES];
-    __shared__ double s_sum[WAVES];
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        most = max(most, (uint32_t)__shfl_xor((int)most, d));
-        sum += __shfl_xor(sum, d);
+// The largest magnitude of a vector and the sum of its squares
+struct Size {
+    uint32_t most = 0;       // bits
+    double squares = 0.0;
+    __device__ void take(float v)
+    {
+        most = max(most, __float_as_uint(v) & 0x7FFFFFFFu);
+        squares = fma((double)v, (double)v, squares);
     }
-    if ((threadIdx.x & 63) == 0) {
-        s_max[threadIdx.x >> 6] = most;
-        s_sum[threadIdx.x >> 6] = sum;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
+    __device__ void take(const float4 &v) { take(v.x); take(v.y); take(v.z); take(v.w); }
+    __device__ void over_wave()
+    {
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) {
-            most = max(most, s_max[w]);
-            sum += s_sum[w];
+        for (int d = 32; d > 0; d >>= 1) {
+            most = max(most, (uint32_t)__shfl_xor((int)most, d));
+            squares += __shfl_xor(squares, d);
         }
     }
-}
+    template <int WAVES>
+    __device__ void over_workgroup()       // (in thread 0)
+    {
+        __shared__ uint32_t s_max[WAVES];
+        __shared__ double s_sum[WAVES];
+        over_wave();
+        if ((threadIdx.x & 63) == 0) {
+            s_max[threadIdx.x >> 6] = most;
+            s_sum[threadIdx.x >> 6] = squares;
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) {
+                most = max(most, s_max[w]);
+                squares += s_sum[w];
+            }
+        }
+    }
+};
 
 __global__ __launch_bounds__(1024) void k_grad_scalings(const float *__restrict__ dY, int rows, Scaling *__restrict__ scalings)
 {
     const float *y = dY + (size_t)blockIdx.x * rows;
-    uint32_t most = 0;
-    double squares = 0.0;
-    auto take = [&](float v) {
-        most = max(most, __float_as_uint(v) & 0x7FFFFFFFu);
-        squares = fma((double)v, (double)v, squares);
-    };
+    Size size;
     if (rows % 4 == 0) {
 #pragma unroll 4
-        for (int r = threadIdx.x * 4; r < rows; r += 4096) {
-            const float4 v = *reinterpret_cast<const float4 *>(y + r);
-            take(v.x); take(v.y); take(v.z); take(v.w);
-        }
+        for (int r = threadIdx.x * 4; r < rows; r += 4096) size.take(*reinterpret_cast<const float4 *>(y + r));
     } else {
-        for (int r = threadIdx.x; r < rows; r += 1024) take(y[r]);
+        for (int r = threadIdx.x; r < rows; r += 1024) size.take(y[r]);
     }
-    over_workgroup<16>(most, squares);
-    if (threadIdx.x == 0) scalings[blockIdx.x] = scaling_of(most, squares, rows);
+    size.over_workgroup<16>();
+    if (threadIdx.x == 0) scalings[blockIdx.x] = scaling_of(size.most, size.squares, rows);
 }
 
 // Gradients of the pre-activations [g; u] of H = act(g) u, and the scalings of their vectors
@@ -92,16 +98,15 @@ __global__ __launch_bounds__(1024) void k_gated_grad(const float *__restrict__ p
     const size_t n = blockIdx.x;
     const float *g = pre + n * 2 * units, *u = g + units, *dh = dH + n * units;
     float *dg = dpre + n * 2 * units, *du = dg + units;
-    uint32_t most = 0;
-    double squares = 0.0;
+    Size size;
     auto one = [&](float g, float u, float dh, float *dg, float *du) {
         float a, da;
         gate_with_slope(gate, g, &a, &da);
         const float x = dh * u * da, y = dh * a;
         *dg = x;
         *du = y;
-        most = max(most, max(__float_as_uint(x) & 0x7FFFFFFFu, __float_as_uint(y) & 0x7FFFFFFFu));
-        squares = fma((double)x, (double)x, fma((double)y, (double)y, squares));
+        size.take(x);
+        size.take(y);
     };
     if (units % 2 == 0) {       // (a vector of 2 units values begins at a multiple of 16 bytes, its second half at one of 8)
 #pragma unroll 2
@@ -117,8 +122,8 @@ __global__ __launch_bounds__(1024) void k_gated_grad(const float *__restrict__ p
     } else {
         for (int r = threadIdx.x; r < units; r += 1024) one(g[r], u[r], dh[r], dg + r, du + r);
     }
-    over_workgroup<16>(most, squares);
-    if (threadIdx.x == 0) scalings[n] = scaling_of(most, squares, 2 * units);
+    size.over_workgroup<16>();
+    if (threadIdx.x == 0) scalings[n] = scaling_of(size.most, size.squares, 2 * units);
 }
 
 // Whether one of the group's vectors needs four digits; the lane's vector is the group's vector lane % 16
@@ -127,15 +132,41 @@ __device__ __forceinline__ bool group_is_wide(const Scaling &mine, bool live) { 
 // The digits in memory: [group of 16 vectors][step of 64 packed rows][digit][lane 16 kb + v][16 bytes], the bytes being the
 // sixteen rows of row tile 4 step + kb of vector v: an operand of a digit of sixteen vectors is 1 KB in one piece.  A wave writes one step.
 // VEC: four rows next to each other in the matrix are four in the tile (one of each gate's units on the gate layout) and aligned to 16 bytes.
-template <bool VEC>
-__global__ __launch_bounds__(256) void k_grad_digits(const float *__restrict__ dY, const Scaling *__restrict__ scalings, int batch, int rows,
-                                                     int gate_h, int steps, int may_narrow, uint8_t *__restrict__ digits)
+// SCALES: every workgroup works the scalings of its sixteen vectors out by itself, a wave each, and the first of them leaves them in memory (a launch
+// less; the vectors are read once per workgroup of sixteen steps).
+template <bool VEC, bool SCALES>
+__global__ __launch_bounds__(SCALES ? 1024 : 256) void k_grad_digits(const float *__restrict__ dY, Scaling *__restrict__ scalings, int batch, int rows,
+                                                                     int gate_h, int steps, int may_narrow, uint8_t *__restrict__ digits)
 {
-    const int lane = threadIdx.x & 63, step = blockIdx.x * 4 + (threadIdx.x >> 6), group = blockIdx.y;
-    if (step >= steps) return;
+    const int lane = threadIdx.x & 63, step = blockIdx.x * (SCALES ? 16 : 4) + (threadIdx.x >> 6), group = blockIdx.y;
     const int n = group * kGroupVectors + (lane & 15), tile = step * 4 + (lane >> 4);
     Scaling sc = {kNotFinite, kNotFinite, 0, 0};
-    if (n < batch) sc = scalings[n];
+    if constexpr (SCALES) {
+        __shared__ Scaling s_scalings[kGroupVectors];
+        const int mine = group * kGroupVectors + (threadIdx.x >> 6);
+        if (mine < batch) {
+            const float *const y = dY + (size_t)mine * rows;
+            Size size;
+            if (rows % 4 == 0) {
+#pragma unroll 4
+                for (int r = lane * 4; r < rows; r += 256) size.take(*reinterpret_cast<const float4 *>(y + r));
+            } else {
+#pragma unroll 4
+                for (int r = lane; r < rows; r += 64) size.take(y[r]);
+            }
+            size.over_wave();
+            if (lane == 0) {
+                const Scaling s = scaling_of(size.most, size.squares, rows);
+                s_scalings[threadIdx.x >> 6] = s;
+                if (blockIdx.x == 0) scalings[mine] = s;
+            }
+        }
+        __syncthreads();
+        if (n < batch) sc = s_scalings[lane & 15];
+    } else {
+        if (n < batch) sc = scalings[n];
+    }
+    if (step >= steps) return;
     const bool narrow = may_narrow && !group_is_wide(sc, n < batch);
     const int e = narrow ? sc.e3 : sc.e4;
     const float *const y = dY + (size_t)n * rows;
@@ -517,21 +548,26 @@ int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, in
     char *const ws = static_cast<char *>(workspace);
     Scaling *const scalings = reinterpret_cast<Scaling *>(ws);
     uint8_t *const digits = reinterpret_cast<uint8_t *>(ws + p.digits_off);
+    // Whether the workgroups of the digits work the scalings out themselves: up to 128 KB of vectors each.  us with it / with a launch of its own:
+    // 1024 x 1024, one vector 12.5 / 14.2; 2000 x 2000, 1000 vectors 35.1 / 37.9; 4096 x 4096, 64 vectors (256 KB) 28.9 / 28.1; 5460 x 1000, 40 (341 KB)
+    // 21.3 / 19.7.
+    const bool own = !gated && (long long)(batch < 16 ? batch : 16) * L.rows <= 32768;
+    int err = 0;
     if (gated) {
         hipLaunchKernelGGL(k_gated_grad, dim3((unsigned)batch), dim3(1024), 0, st, gated->pre, gated->dH, L.rows / 2, gated->gate, gated->dpre,
                            scalings);
         dY = gated->dpre;
-    } else {
+    } else if (!own) {
         hipLaunchKernelGGL(k_grad_scalings, dim3((unsigned)batch), dim3(1024), 0, st, dY, L.rows, scalings);
     }
-    int err = (int)hipGetLastError();
+    err = (int)hipGetLastError();
     if (err) return err;
-    const dim3 by_steps((unsigned)((p.steps + 3) / 4), (unsigned)((batch + 15) / 16));
-    const int may_narrow = p.wm >= 4;
-    if ((L.gate_h ? L.gate_h : L.rows) % 4 == 0)
-        hipLaunchKernelGGL(k_grad_digits<true>, by_steps, dim3(256), 0, st, dY, scalings, batch, L.rows, L.gate_h, p.steps, may_narrow, digits);
-    else
-        hipLaunchKernelGGL(k_grad_digits<false>, by_steps, dim3(256), 0, st, dY, scalings, batch, L.rows, L.gate_h, p.steps, may_narrow, digits);
+    const int waves = own ? 16 : 4, may_narrow = p.wm >= 4;
+    const bool vec = (L.gate_h ? L.gate_h : L.rows) % 4 == 0;
+    hipLaunchKernelGGL(vec ? (own ? k_grad_digits<true, true> : k_grad_digits<true, false>)
+                           : (own ? k_grad_digits<false, true> : k_grad_digits<false, false>),
+                       dim3((unsigned)((p.steps + waves - 1) / waves), (unsigned)((batch + 15) / 16)), dim3((unsigned)waves * 64), 0, st, dY,
+                       scalings, batch, L.rows, L.gate_h, p.steps, may_narrow, digits);
     err = (int)hipGetLastError();
     if (err) return err;
     GradArgs a;

@@ -134,7 +134,7 @@ def lib():
         binding, why_not = _use_binding()   # (once more: it may have been built since this module was imported)
         if binding is not None:
             binding.bind(pb_desc, pb_adapters, PbError,
-                         {n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in _NATIVE + _NATIVE_OPERATORS})
+                         {n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in _NATIVE + _NATIVE_OPERATORS + _SIZES})
         else:
             warnings.warn("calls go through ctypes, 6 to 8 us slower each: %s (python -m paper_2003_00822_amd.build)"
                           % why_not, RuntimeWarning, stacklevel=2)
@@ -413,18 +413,38 @@ class PackedLinear:
               keep: bool = False):
         """H = act(g) u with [g; u] = W x + bias: the block's two projections packed as one matrix, gate rows first.  With `keep` also the
         pre-activations [g; u], for gated_grad."""
+        return _methods["gated"](self, X, gate, bits_used, bias, keep)
+
+    def gated_grad(self, pre: torch.Tensor, dH: torch.Tensor, gate: int = PB_GATE_SILU, bits_used: int | None = None):
+        """(dX, dpre) of `gated`, from the pre-activations that it kept."""
+        return _methods["gated_grad"](self, pre, dH, gate, bits_used)
+
+    def grad(self, dY: torch.Tensor, bits_used: int | None = None):
+        """dX = dY W: the gradient of the layer's activations, through the first `bits_used` bitlayers."""
+        return _methods["grad"](self, dY, bits_used)
+
+    def adapted(self, X: torch.Tensor, adapters: Adapters, index: torch.Tensor | None, bits_used: int | None = None,
+                bias: torch.Tensor | None = None):
+        """W x + bias + scale_k B_k A_k x with k = index[n] (int32; outside [0, count): no adapter; None: adapter 0 for all)."""
+        return _methods["adapted"](self, X, adapters, index, bits_used, bias)
+
+    def adapted_grad(self, X: torch.Tensor, dY: torch.Tensor, adapters: Adapters, index: torch.Tensor | None, bits_used: int | None = None,
+                     inputs: bool = True):
+        """(dX, dA, dB) of `adapted`, all fp32; dX is None without `inputs`."""
+        return _methods["adapted_grad"](self, X, dY, adapters, index, bits_used, inputs)
+
+    def _gated_checked(self, X, gate, bits_used, bias, keep):
         X = self._vectors(X, self.cols, "X")
         n = X.shape[0]
+        self._sized(bias, "bias", (self.rows,))
         with self._here(X, bias):
             H = torch.empty((n, self.rows // 2), dtype=torch.float32, device=X.device)
             pre = torch.empty((n, self.rows), dtype=torch.float32, device=X.device) if keep else None
-            self._sized(bias, "bias", (self.rows,))
             pb_gated_linear(self.packed, self.scales, self.desc, self.bits if bits_used is None else bits_used, X, n, bias, gate, H, pre,
                             self._work(pb_workspace_bytes(self.desc, n)))
         return (H, pre) if keep else H
 
-    def gated_grad(self, pre: torch.Tensor, dH: torch.Tensor, gate: int = PB_GATE_SILU, bits_used: int | None = None):
-        """(dX, dpre) of `gated`, from the pre-activations that it kept."""
+    def _gated_grad_checked(self, pre, dH, gate, bits_used):
         pre, dH = self._vectors(pre, self.rows, "pre"), self._vectors(dH, self.rows // 2, "dH")
         n = pre.shape[0]
         self._sized(dH, "dH", (n, self.rows // 2))
@@ -435,8 +455,7 @@ class PackedLinear:
                                  self._work(pb_grad_workspace_bytes(self.desc, n)))
         return dX, dpre
 
-    def grad(self, dY: torch.Tensor, bits_used: int | None = None):
-        """dX = dY W: the gradient of the layer's activations, through the first `bits_used` bitlayers."""
+    def _grad_checked(self, dY, bits_used):
         dY = self._vectors(dY, self.rows, "dY")
         n = dY.shape[0]
         with self._here(dY):
@@ -445,28 +464,24 @@ class PackedLinear:
                            self._work(pb_grad_workspace_bytes(self.desc, n)))
         return dX
 
-    def adapted(self, X: torch.Tensor, adapters: Adapters, index: torch.Tensor | None, bits_used: int | None = None,
-                bias: torch.Tensor | None = None):
-        """W x + bias + scale_k B_k A_k x with k = index[n] (int32; outside [0, count): no adapter; None: adapter 0 for all)."""
+    def _adapted_checked(self, X, adapters, index, bits_used, bias):
         X = self._vectors(X, self.cols, "X")
         n = X.shape[0]
         self._sized(index, "index", (n,))
         self._sized(bias, "bias", (self.rows,))
-        with self._here(X, index, bias, adapters.A):
+        with self._here(X, index, bias, adapters.A, adapters.B, adapters.scale):
             desc = self._desc_of(adapters)
             Y = torch.empty((n, self.rows), dtype=torch.float32, device=X.device)
             pb_matmul_adapters(self.packed, self.scales, self.desc, self.bits if bits_used is None else bits_used, X, n, desc, index, bias, Y,
                                self._work(pb_adapters_workspace_bytes(self.desc, desc, n)))
         return Y
 
-    def adapted_grad(self, X: torch.Tensor, dY: torch.Tensor, adapters: Adapters, index: torch.Tensor | None, bits_used: int | None = None,
-                     inputs: bool = True):
-        """(dX, dA, dB) of `adapted`, all fp32; dX is None without `inputs`."""
+    def _adapted_grad_checked(self, X, dY, adapters, index, bits_used, inputs):
         X, dY = self._vectors(X, self.cols, "X"), self._vectors(dY, self.rows, "dY")
         n = X.shape[0]
         self._sized(dY, "dY", (n, self.rows))
         self._sized(index, "index", (n,))
-        with self._here(X, dY, index, adapters.A):
+        with self._here(X, dY, index, adapters.A, adapters.B, adapters.scale):
             desc = self._desc_of(adapters)
             dX = torch.empty((n, self.cols), dtype=torch.float32, device=X.device) if inputs else None
             dA = torch.empty(adapters.A.shape, dtype=torch.float32, device=X.device)
@@ -513,8 +528,11 @@ _NATIVE = ["pb_quantize_pack", "pb_quantize_pack_desc", "pb_quantize_pack_mode",
            "pb_matmul_static", "pb_matmul_bias_act", "pb_matmul_acc", "pb_matmul_acc_pairs", "pb_act_prep",
            "pb_matmul_prepared", "pb_fixed_point", "pb_lstm_cell"]
 _NATIVE_OPERATORS = ["pb_gated_linear", "pb_matmul_grad", "pb_gated_linear_grad", "pb_matmul_adapters", "pb_matmul_adapters_grad"]
+_SIZES = ["pb_workspace_bytes", "pb_grad_workspace_bytes", "pb_adapters_workspace_bytes"]
 _linear = PackedLinear._call_checked
-_PYTHON = {**{n: globals()[n] for n in _NATIVE + _NATIVE_OPERATORS}, "linear": _linear}
+# PackedLinear's operators, by their names
+_methods = {n: getattr(PackedLinear, "_%s_checked" % n) for n in ("gated", "gated_grad", "grad", "adapted", "adapted_grad")}
+_PYTHON = {**{n: globals()[n] for n in _NATIVE + _NATIVE_OPERATORS}, "linear": _linear, **_methods}
 
 
 def _use_binding():
@@ -527,11 +545,12 @@ def _use_binding():
     here = "%s %s" % (torch.__version__, sys.implementation.cache_tag)
     if getattr(binding, "BUILT_FOR", None) != here:   # (it takes tensors apart by torch's headers)
         return None, "the native binding is built for %s, not for %s" % (getattr(binding, "BUILT_FOR", "?"), here)
-    if not all(hasattr(binding, n) for n in _NATIVE + _NATIVE_OPERATORS):
+    if not all(hasattr(binding, n) for n in [*_NATIVE, *_NATIVE_OPERATORS, *_methods]):
         return None, "the native binding is built from other sources"
     binding.set_slow(_PYTHON)
     globals().update({n: getattr(binding, n) for n in _NATIVE + _NATIVE_OPERATORS})
     globals()["_linear"] = binding.linear
+    globals()["_methods"] = {n: getattr(binding, n) for n in _methods}
     return binding, None
 
 

@@ -614,3 +614,46 @@ def test_outputs_and_nothing_else_are_written(pb):
     pb.pb_gated_linear_grad(lin.packed, lin.scales, d, 8, pre, H, n, 1, dpre, dX, ws)
     check(ws, size, (dpre, n), (dX, n))
     assert torch.equal(X.cpu(), c.X) and torch.equal(dY.cpu(), c.dY) and torch.equal(index.cpu(), c.index)
+
+
+@pytest.mark.gpu
+def test_native_and_python_operators_agree(pb):
+    """The native forms of PackedLinear's operators against the Python functions behind them, unusual arguments to both, and stand-ins for the tensors."""
+    if not isinstance(pb.pb_matmul, type(len)):
+        pytest.skip("no native binding")
+    b = Block(pb)
+    bias, none = torch.randn(600, device="cuda"), torch.full((24,), -1, dtype=torch.int32, device="cuda")
+    H, pre = b.up.gated(b.X, keep=True)
+    calls = [
+        ("gated", b.up, (b.X, 1, None, None, False)), ("gated", b.up, (b.X, 2, 5, bias, True)), ("gated", b.up, (b.X[5], 0, 8, None, True)),
+        ("gated_grad", b.up, (pre, H, 1, None)), ("gated_grad", b.up, (pre.reshape(4, 6, 600), H, 3, 4)),
+        ("grad", b.down, (b.dY, None)), ("grad", b.down, (b.dY[2], 3)),
+        ("adapted", b.down, (H, b.adapters, b.index, None, None)), ("adapted", b.down, (H, b.adapters, None, 6, bias[:200].clone())),
+        ("adapted", b.down, (H, pb.Adapters(b.adapters.A.float(), b.adapters.B.float()), none, None, None)),
+        ("adapted_grad", b.down, (H, b.dY, b.adapters, b.index, None, True)), ("adapted_grad", b.down, (H, b.dY, b.adapters, None, 7, False)),
+    ]
+    for name, layer, args in calls:
+        native, python = pb._methods[name](layer, *args), pb._PYTHON[name](layer, *args)
+        native, python = ([t] if isinstance(t, torch.Tensor) else list(t) for t in (native, python))
+        assert len(native) == len(python)
+        for x, y in zip(native, python):
+            assert (x is None and y is None) or torch.equal(x, y), name
+    for name, layer, args, error in (
+            ("gated", b.up, (b.X.double(), 1, None, None, False), TypeError), ("gated", b.up, (b.X.cpu(), 1, None, None, False), ValueError),
+            ("gated", b.up, (b.X, 1, None, bias[:5], False), ValueError), ("gated", b.up, (b.X, 1, 9, None, False), pb.PbError),
+            ("grad", b.down, (b.dY[:0], None), pb.PbError), ("adapted", b.down, (H, b.adapters, b.index.cpu(), None, None), ValueError),
+            ("adapted_grad", b.down, (H, b.dY[:3], b.adapters, b.index, None, True), ValueError)):
+        for f in (pb._methods[name], pb._PYTHON[name]):
+            with pytest.raises(error):
+                f(layer, *args)
+    # the tensors that an optimizer puts in the place of others are the ones that count
+    want = b.down.adapted(H, b.adapters, b.index)
+    A = b.adapters.A
+    b.adapters.A = torch.zeros_like(A)
+    plain = b.down.adapted(H, b.adapters, none)
+    assert torch.equal(b.down.adapted(H, b.adapters, b.index), plain) and not torch.equal(plain, want)
+    b.adapters.A = A
+    assert torch.equal(b.down.adapted(H, b.adapters, b.index), want)
+    b.adapters.A = A[:, :, :10].contiguous()
+    with pytest.raises(ValueError, match="another type or shape"):
+        b.down.adapted(H, b.adapters, b.index)
