@@ -25,38 +25,41 @@ struct f16 { uint16_t v; };
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(bf16 v) { return __uint_as_float((uint32_t)v.v << 16); }
 __device__ __forceinline__ float to_f32(f16 v) { return (float)__builtin_bit_cast(_Float16, v.v); }
-// Four values next to each other (aligned to their size)
-__device__ __forceinline__ v4f load4(const float *p) { return *reinterpret_cast<const v4f *>(p); }
+// Four values next to each other.  Global memory takes loads and stores of 8 and 16 bytes at any multiple of a value's size.
+typedef float v4f_at4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_at2 __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ v4f load4(const float *p) { return *reinterpret_cast<const v4f_at4 *>(p); }
 __device__ __forceinline__ v4f load4(const bf16 *p)
 {
-    const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
+    const u32x2 w = *reinterpret_cast<const u32x2_at2 *>(p);
     return v4f{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xFFFF0000u), __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xFFFF0000u)};
 }
 __device__ __forceinline__ v4f load4(const f16 *p)
 {
-    const u32x2 w = *reinterpret_cast<const u32x2 *>(p);
+    const u32x2 w = *reinterpret_cast<const u32x2_at2 *>(p);
     return v4f{to_f32(f16{(uint16_t)w[0]}), to_f32(f16{(uint16_t)(w[0] >> 16)}), to_f32(f16{(uint16_t)w[1]}), to_f32(f16{(uint16_t)(w[1] >> 16)})};
 }
-// The values p[at .. at + 4) of `length`, 0 beyond the end.  VEC: `length` and `at` are multiples of four.
-template <bool VEC, typename T>
+// The values p[at .. at + 4) of `length`, 0 beyond the end
+template <typename T>
 __device__ __forceinline__ v4f load4_of(const T *p, int at, int length)
 {
-    if constexpr (VEC) return at < length ? load4(p + at) : v4f{0, 0, 0, 0};
-    else {
-        v4f v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = at + i < length ? to_f32(p[at + i]) : 0.0f;
-        return v;
-    }
-}
-template <bool VEC>
-__device__ __forceinline__ void store4_of(float *p, int at, int length, v4f v)
-{
-    if constexpr (VEC) {
-        if (at < length) *reinterpret_cast<v4f *>(p + at) = v;
+    v4f v = {0, 0, 0, 0};
+    if (at + 4 <= length) {
+        v = load4(p + at);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 3; ++i)
+            if (at + i < length) v[i] = to_f32(p[at + i]);
+    }
+    return v;
+}
+__device__ __forceinline__ void store4_of(float *p, int at, int length, v4f v)
+{
+    if (at + 4 <= length) {
+        *reinterpret_cast<v4f_at4 *>(p + at) = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
             if (at + i < length) p[at + i] = v[i];
     }
 }
@@ -235,7 +238,7 @@ struct DownArgs {
 // Parts of the sum of a tile's products go to the waves of `slices` workgroups; a lane's result is four ranks of one vector.
 //   TURNED: the summands are the rows of the matrix (B: [length][rank]), else its columns (A: [rank][length])
 constexpr int kDownWaves = 8;
-template <typename T, bool TURNED, bool VEC, int RT>
+template <typename T, bool TURNED, int RT>
 __device__ __forceinline__ void adapter_down(const DownArgs &a, int rt0, v4f (*s_part)[RT][64])
 {
     const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
@@ -249,7 +252,7 @@ __device__ __forceinline__ void adapter_down(const DownArgs &a, int rt0, v4f (*s
     for (int c0 = (blockIdx.y * kDownWaves + wave) * 64; c0 < a.length; c0 += a.slices * kDownWaves * 64) {
         v4f v[4], w[4][RT];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = load4_of<VEC>(x, c0 + 16 * q + 4 * kb, a.length);
+        for (int q = 0; q < 4; ++q) v[q] = load4_of(x, c0 + 16 * q + 4 * kb, a.length);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int c = c0 + 16 * q + 4 * kb;
@@ -262,7 +265,7 @@ __device__ __forceinline__ void adapter_down(const DownArgs &a, int rt0, v4f (*s
 #pragma unroll
                         for (int e = 0; e < 4; ++e) w[q][t][e] = c + e < a.length ? to_f32(M[(size_t)(c + e) * a.rank + j]) : 0.0f;
                     } else {
-                        w[q][t] = load4_of<VEC>(M + (size_t)j * a.length, c, a.length);
+                        w[q][t] = load4_of(M + (size_t)j * a.length, c, a.length);
                     }
                 }
             }
@@ -296,13 +299,13 @@ __device__ __forceinline__ void adapter_down(const DownArgs &a, int rt0, v4f (*s
     }
 }
 // u, t or both
-template <typename T, bool VEC_X, bool VEC_DY, int RT>
+template <typename T, int RT>
 __global__ __launch_bounds__(kDownWaves * 64) void k_adapter_down(const DownArgs u, const DownArgs t)
 {
     __shared__ v4f s_part[kDownWaves - 1][RT][64];
     const int z = blockIdx.z * RT;
-    if (u.V && z < u.ranks) adapter_down<T, false, VEC_X, RT>(u, z, s_part);
-    else adapter_down<T, true, VEC_DY, RT>(t, u.V ? z - (u.ranks + RT - 1) / RT * RT : z, s_part);
+    if (u.V && z < u.ranks) adapter_down<T, false, RT>(u, z, s_part);
+    else adapter_down<T, true, RT>(t, u.V ? z - (u.ranks + RT - 1) / RT * RT : z, s_part);
 }
 // Ranks 4 part .. 4 part + 3 of rank tile `rt` of a vector: the slices added up in their order
 __device__ __forceinline__ v4f down_at(const float *parts, int slices, int batch, int ranks, int vector, int rt, int part)
@@ -330,7 +333,7 @@ struct UpArgs {
     int length, rank, ranks, slices, blocks;
 };
 // A wave does `blocks` times 64 values of the tile's vectors.  RT rank tiles at once.  TURNED: M is A [rank][length], else B [length][rank]
-template <typename T, bool TURNED, bool VEC, bool RANK4, int RT>
+template <typename T, bool TURNED, int RT>
 __global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
 {
     const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
@@ -365,7 +368,7 @@ __global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
     v4f before[4];
     auto load_before = [&](int r0) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) before[t] = load4_of<VEC>(y, value_at(r0, t), end);
+        for (int t = 0; t < 4; ++t) before[t] = load4_of(y, value_at(r0, t), end);
     };
     load_before(first);
     load_u(0);
@@ -383,10 +386,10 @@ __global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
                     w[x][t] = v4f{0, 0, 0, 0};
                     if constexpr (TURNED) {      // t: summand 4 t + kb, four values (in the order in which a lane's results then are four and four)
                         const int j = (rt0 + x) * 16 + 4 * t + kb;
-                        if (j < a.rank) w[x][t] = load4_of<VEC>(M + (size_t)j * a.length, r0 + 16 * (i & 3) + 4 * (i >> 2), a.length);
+                        if (j < a.rank) w[x][t] = load4_of(M + (size_t)j * a.length, r0 + 16 * (i & 3) + 4 * (i >> 2), a.length);
                     } else {                     // t: value r0 + 16 t + i, the summands 4 kb .. 4 kb + 3
                         const int r = r0 + 16 * t + i;
-                        if (r < a.length) w[x][t] = load4_of<RANK4>(M + (size_t)r * a.rank, (rt0 + x) * 16 + 4 * kb, a.rank);
+                        if (r < a.length) w[x][t] = load4_of(M + (size_t)r * a.rank, (rt0 + x) * 16 + 4 * kb, a.rank);
                     }
                 }
 #pragma unroll
@@ -408,7 +411,7 @@ __global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
             for (int t = 0; t < 4; ++t) {
                 v4f v = acc[t];
                 if constexpr (TURNED) v = v4f{acc[0][t], acc[1][t], acc[2][t], acc[3][t]};
-                store4_of<VEC>(y, value_at(r0, t), end, now[t] + v);
+                store4_of(y, value_at(r0, t), end, now[t] + v);
             }
         }
     }
@@ -425,7 +428,7 @@ struct OuterArgs {
 };
 constexpr int kOuterWaves = 8;
 // A workgroup does 64 columns (rows) and RT rank tiles of an adapter; its waves take every eighth four of the adapter's vectors.
-template <bool TURNED, bool VEC, bool RANK4, int RT>
+template <bool TURNED, int RT>
 __device__ __forceinline__ void adapter_outer(const OuterArgs &a, int block, v4f (*s_part)[RT * 4][64])
 {
     const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
@@ -450,7 +453,7 @@ __device__ __forceinline__ void adapter_outer(const OuterArgs &a, int block, v4f
         }
 #pragma unroll
         for (int x = 0; x < AT_ONCE; ++x) {
-            v[x] = n[x] >= 0 ? load4_of<VEC>(a.V + (size_t)n[x] * a.length, c, a.length) : v4f{0, 0, 0, 0};
+            v[x] = n[x] >= 0 ? load4_of(a.V + (size_t)n[x] * a.length, c, a.length) : v4f{0, 0, 0, 0};
 #pragma unroll
             for (int t = 0; t < RT; ++t)
                 u[x][t] = n[x] >= 0 && rt0 + t < a.ranks ? down1_at(a.parts, a.slices, a.order.batch, a.ranks, n[x], rt0 + t, i) : 0.0f;
@@ -483,24 +486,24 @@ __device__ __forceinline__ void adapter_outer(const OuterArgs &a, int block, v4f
         if constexpr (TURNED) {
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                if (c + q < a.length) store4_of<RANK4>(a.out + ((size_t)k * a.length + c + q) * a.rank, j, a.rank, acc[t][q]);
+                if (c + q < a.length) store4_of(a.out + ((size_t)k * a.length + c + q) * a.rank, j, a.rank, acc[t][q]);
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (j + e < a.rank)
-                    store4_of<VEC>(a.out + ((size_t)k * a.rank + j + e) * a.length, c, a.length, v4f{acc[t][0][e], acc[t][1][e], acc[t][2][e], acc[t][3][e]});
+                    store4_of(a.out + ((size_t)k * a.rank + j + e) * a.length, c, a.length, v4f{acc[t][0][e], acc[t][1][e], acc[t][2][e], acc[t][3][e]});
         }
     }
 }
 
 // dA, dB or both
-template <bool VEC_X, bool VEC_DY, bool RANK4, int RT>
+template <int RT>
 __global__ __launch_bounds__(kOuterWaves * 64) void k_adapter_outer(const OuterArgs A, const OuterArgs B)
 {
     __shared__ v4f s_part[kOuterWaves - 1][RT * 4][64];
     const int block = blockIdx.x, of_A = A.out ? (A.length + 63) / 64 : 0;
-    if (block < of_A) adapter_outer<false, VEC_X, RANK4, RT>(A, block, s_part);
-    else adapter_outer<true, VEC_DY, RANK4, RT>(B, block - of_A, s_part);
+    if (block < of_A) adapter_outer<false, RT>(A, block, s_part);
+    else adapter_outer<true, RT>(B, block - of_A, s_part);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -566,29 +569,6 @@ static int launch(const void *fn, dim3 grid, int threads, void *args, hipStream_
     const hipError_t e = hipLaunchKernel(fn, grid, dim3((unsigned)threads), list, 0, st);
     return (int)(e != hipSuccess ? e : hipGetLastError());
 }
-// The kernel for two truth values
-template <template <bool, bool> class K>
-static const void *by_two(bool a, bool b)
-{
-    if (a) return b ? K<true, true>::fn() : K<true, false>::fn();
-    return b ? K<false, true>::fn() : K<false, false>::fn();
-}
-template <typename T, int RT>
-struct Down {
-    template <bool X, bool DY>
-    struct K { static const void *fn() { return reinterpret_cast<const void *>(k_adapter_down<T, X, DY, RT>); } };
-};
-template <typename T, bool TURNED, int RT>
-struct Up {
-    // (the rank of A's rows does not matter)
-    template <bool VEC, bool RANK4>
-    struct K { static const void *fn() { return reinterpret_cast<const void *>(k_adapter_up<T, TURNED, VEC, TURNED || RANK4, RT>); } };
-};
-template <bool RANK4, int RT>
-struct Outer {
-    template <bool X, bool DY>
-    struct K { static const void *fn() { return reinterpret_cast<const void *>(k_adapter_outer<X, DY, RANK4, RT>); } };
-};
 static int launch_two(const void *fn, dim3 grid, int threads, void *first, void *second, hipStream_t st)
 {
     void *list[] = {first, second};
@@ -607,11 +587,10 @@ int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layou
     t = u;
     u.M = ad.A; u.scale = nullptr; u.V = X; u.length = L.cols; u.out = reinterpret_cast<float *>(ws + p.u_off);
     t.M = ad.B; t.scale = ad.scale; t.V = dY; t.length = L.rows; t.out = reinterpret_cast<float *>(ws + p.t_off);
-    const bool vx = L.cols % 4 == 0, vy = L.rows % 4 == 0;
     return by_type(ad.type, [&](auto type) {
         typedef decltype(type) T;
-        const void *fn = rt == 1 ? by_two<Down<T, 1>::template K>(vx, vy)
-                                 : (rt == 2 ? by_two<Down<T, 2>::template K>(vx, vy) : by_two<Down<T, 4>::template K>(vx, vy));
+        const void *fn = rt == 1 ? reinterpret_cast<const void *>(k_adapter_down<T, 1>)
+                                 : (rt == 2 ? reinterpret_cast<const void *>(k_adapter_down<T, 2>) : reinterpret_cast<const void *>(k_adapter_down<T, 4>));
         return launch_two(fn, dim3((unsigned)p.items, (unsigned)p.slices, (unsigned)(z * ((X ? 1 : 0) + (dY ? 1 : 0)))), kDownWaves * 64, &u, &t, st);
     });
 }
@@ -633,11 +612,10 @@ static int launch_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &
     const long long waves = (long long)((a.length + 63) / 64) * p.items;
     a.blocks = waves < 2 * 4096 ? 1 : (waves < 4 * 4096 ? 2 : 4);
     const int rt = p.ranks >= 3 ? 4 : p.ranks;
-    const bool vec = a.length % 4 == 0, rank4 = TURNED || ad.rank % 4 == 0;
     return by_type(ad.type, [&](auto type) {
         typedef decltype(type) T;
-        const void *fn = rt == 1 ? by_two<Up<T, TURNED, 1>::template K>(vec, rank4)
-                                 : (rt == 2 ? by_two<Up<T, TURNED, 2>::template K>(vec, rank4) : by_two<Up<T, TURNED, 4>::template K>(vec, rank4));
+        const void *fn = rt == 1 ? reinterpret_cast<const void *>(k_adapter_up<T, TURNED, 1>)
+                                 : (rt == 2 ? reinterpret_cast<const void *>(k_adapter_up<T, TURNED, 2>) : reinterpret_cast<const void *>(k_adapter_up<T, TURNED, 4>));
         return launch(fn, dim3((unsigned)((a.length + 256 * a.blocks - 1) / (256 * a.blocks)), (unsigned)p.items), 256, &a, st);
     });
 }
@@ -663,10 +641,8 @@ int launch_adapter_grads(const AdapterPlan &p, const pb_adapters &ad, const Layo
     B = A;
     A.scale = nullptr; A.parts = reinterpret_cast<const float *>(ws + p.t_off); A.V = X; A.out = dA; A.length = L.cols;
     B.scale = ad.scale; B.parts = reinterpret_cast<const float *>(ws + p.u_off); B.V = dY; B.out = dB; B.length = L.rows;
-    const bool vx = L.cols % 4 == 0, vy = L.rows % 4 == 0, rank4 = ad.rank % 4 == 0;
     const int rt = p.ranks == 1 ? 1 : 2;
-    const void *fn = rt == 1 ? (rank4 ? by_two<Outer<true, 1>::K>(vx, vy) : by_two<Outer<false, 1>::K>(vx, vy))
-                             : (rank4 ? by_two<Outer<true, 2>::K>(vx, vy) : by_two<Outer<false, 2>::K>(vx, vy));
+    const void *fn = rt == 1 ? reinterpret_cast<const void *>(k_adapter_outer<1>) : reinterpret_cast<const void *>(k_adapter_outer<2>);
     const int blocks = (dA ? (L.cols + 63) / 64 : 0) + (dB ? (L.rows + 63) / 64 : 0);
     return launch_two(fn, dim3((unsigned)blocks, (unsigned)ad.count, (unsigned)((p.ranks + rt - 1) / rt)), kOuterWaves * 64, &A, &B, st);
 }

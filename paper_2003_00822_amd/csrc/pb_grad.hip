@@ -6,8 +6,9 @@
 // 0x808080 = sum_(d < 3) 256^d 128.  The rounding (half a unit, at most 2^-30 of the vector's largest gradient) is the only one before the last
 // step: |s code| <= 2^14, so a sum over 65536 rows is exact in int32, and the digits' sums are put together in fp64.
 // Batches, which the matrix instructions bound, take three digits (half a unit: at most 2^-23 of the largest gradient) where no vector of
-// sixteen has a value above 12 times the root of its mean square: a result is then off by 12 * 2^-22 / sqrt(12) = 8e-7 of the results' root
-// mean square at most, typically a quarter of it, which is what a product in fp32 is off by.
+// sixteen has a value above 12 sqrt(max(1, R / 4096)) times the root of its mean square: a result over R rows is then off by
+// 12 * 2^-22 / sqrt(12) = 8e-7 sqrt(max(1, R / 4096)) of the results' root mean square at most, typically a quarter of it.  (A product in fp32 is
+// off by 1.75e-8 sqrt(R), measured from 1500 to 21844 rows: 1.1e-6 at 4096.)
 //
 // The sum runs over the rows of W, and a packed word holds 32 columns of one row: the codes have to be turned, 16 rows of a column
 // into the 16 bytes of a lane.  They go through LDS anyway, because every wave needs them, and DS_READ_B64_TR_B8 turns them on the
@@ -20,6 +21,7 @@ namespace pb {
 
 typedef int v2i __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float float4_at4 __attribute__((ext_vector_type(4), aligned(4)));     // (global memory takes loads of 16 bytes at any multiple of four)
 
 constexpr int kNotFinite = INT32_MIN;      // in the place of an exponent: the vector's results are NaN
 
@@ -35,7 +37,7 @@ __device__ __forceinline__ Scaling scaling_of(uint32_t largest, double squares, 
     const double most = (double)__uint_as_float(largest);
     const float f = frexpf(__uint_as_float(largest), &e);
     // (three balanced digits hold 127 * 65536 + 127 * 256 + 127 = 8355711 < 2^23)
-    return {30 - e, 23 - e - (f * 8388608.0f > 8355000.0f ? 1 : 0), most * most * count > 144.0 * squares ? 1 : 0, 0};
+    return {30 - e, 23 - e - (f * 8388608.0f > 8355000.0f ? 1 : 0), most * most * count > 144.0 * fmax(1.0, count / 4096.0) * squares ? 1 : 0, 0};
 }
 
 // The largest magnitude of a vector and the sum of its squares
@@ -47,7 +49,17 @@ struct Size {
         most = max(most, __float_as_uint(v) & 0x7FFFFFFFu);
         squares = fma((double)v, (double)v, squares);
     }
-    __device__ void take(const float4 &v) { take(v.x); take(v.y); take(v.z); take(v.w); }
+    // thread `first` of `threads`: its share of y[0 .. rows)
+    __device__ void take(const float *y, int rows, int first, int threads)
+    {
+        const int fours = rows / 4;
+#pragma unroll 4
+        for (int i = first; i < fours; i += threads) {
+            const float4_at4 v = *reinterpret_cast<const float4_at4 *>(y + 4 * i);
+            take(v.x); take(v.y); take(v.z); take(v.w);
+        }
+        if (first < rows - 4 * fours) take(y[4 * fours + first]);
+    }
     __device__ void over_wave()
     {
 #pragma unroll
@@ -81,12 +93,7 @@ __global__ __launch_bounds__(1024) void k_grad_scalings(const float *__restrict_
 {
     const float *y = dY + (size_t)blockIdx.x * rows;
     Size size;
-    if (rows % 4 == 0) {
-#pragma unroll 4
-        for (int r = threadIdx.x * 4; r < rows; r += 4096) size.take(*reinterpret_cast<const float4 *>(y + r));
-    } else {
-        for (int r = threadIdx.x; r < rows; r += 1024) size.take(y[r]);
-    }
+    size.take(y, rows, threadIdx.x, 1024);
     size.over_workgroup<16>();
     if (threadIdx.x == 0) scalings[blockIdx.x] = scaling_of(size.most, size.squares, rows);
 }
@@ -131,10 +138,9 @@ __device__ __forceinline__ bool group_is_wide(const Scaling &mine, bool live) { 
 
 // The digits in memory: [group of 16 vectors][step of 64 packed rows][digit][lane 16 kb + v][16 bytes], the bytes being the
 // sixteen rows of row tile 4 step + kb of vector v: an operand of a digit of sixteen vectors is 1 KB in one piece.  A wave writes one step.
-// VEC: four rows next to each other in the matrix are four in the tile (one of each gate's units on the gate layout) and aligned to 16 bytes.
 // SCALES: every workgroup works the scalings of its sixteen vectors out by itself, a wave each, and the first of them leaves them in memory (a launch
 // less; the vectors are read once per workgroup of sixteen steps).
-template <bool VEC, bool SCALES>
+template <bool SCALES>
 __global__ __launch_bounds__(SCALES ? 1024 : 256) void k_grad_digits(const float *__restrict__ dY, Scaling *__restrict__ scalings, int batch, int rows,
                                                                      int gate_h, int steps, int may_narrow, uint8_t *__restrict__ digits)
 {
@@ -147,13 +153,7 @@ __global__ __launch_bounds__(SCALES ? 1024 : 256) void k_grad_digits(const float
         if (mine < batch) {
             const float *const y = dY + (size_t)mine * rows;
             Size size;
-            if (rows % 4 == 0) {
-#pragma unroll 4
-                for (int r = lane * 4; r < rows; r += 256) size.take(*reinterpret_cast<const float4 *>(y + r));
-            } else {
-#pragma unroll 4
-                for (int r = lane; r < rows; r += 64) size.take(y[r]);
-            }
+            size.take(y, rows, lane, 64);
             size.over_wave();
             if (lane == 0) {
                 const Scaling s = scaling_of(size.most, size.squares, rows);
@@ -170,27 +170,25 @@ __global__ __launch_bounds__(SCALES ? 1024 : 256) void k_grad_digits(const float
     const bool narrow = may_narrow && !group_is_wide(sc, n < batch);
     const int e = narrow ? sc.e3 : sc.e4;
     const float *const y = dY + (size_t)n * rows;
+    // (four rows of the tile are next to each other in the matrix; on the gate layout the units 4 t .. 4 t + 3 of a gate, rows 4 (unit) + gate of tile t)
     float v[16];
-    if constexpr (VEC) {
-        // (row tile t on the gate layout: units 4 t .. 4 t + 3 of each gate, row 4 (unit) + gate of the tile)
-        const int height = gate_h ? gate_h : rows;
+    const int height = gate_h ? gate_h : rows;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int r = gate_h ? tile * 4 : tile * kTileRows + 4 * k;
-            float4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (e != kNotFinite && r < height) x = *reinterpret_cast<const float4 *>(y + (gate_h ? (size_t)k * gate_h : 0) + r);
-            const float xs[4] = {x.x, x.y, x.z, x.w};
+    for (int k = 0; k < 4; ++k) {
+        const int r = gate_h ? tile * 4 : tile * kTileRows + 4 * k;
+        const float *const at = y + (gate_h ? (size_t)k * gate_h : 0) + r;
+        float4_at4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (e != kNotFinite && r + 4 <= height) {
+            x = *reinterpret_cast<const float4_at4 *>(at);
+        } else if (e != kNotFinite) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (gate_h) v[4 * i + k] = xs[i];
-                else v[4 * k + i] = xs[i];
-            }
+            for (int i = 0; i < 3; ++i)
+                if (r + i < height) x[i] = at[i];
         }
-    } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int r = gate_h ? gates_matrix_row(tile * kTileRows + i, gate_h) : tile * kTileRows + i;
-            v[i] = e != kNotFinite && r >= 0 && r < rows ? y[r] : 0.0f;
+        for (int i = 0; i < 4; ++i) {
+            if (gate_h) v[4 * i + k] = x[i];
+            else v[4 * k + i] = x[i];
         }
     }
     const int balance = narrow ? 0x8080 : 0x808080;
@@ -244,8 +242,8 @@ struct GradArgs {
 // columns each.  Its codes are in two buffers of 64 KB: `columns` of a chunk's 512 and as many row tiles as fit.
 template <int WM>
 struct GradShape {
-    static constexpr int WN = WM >= 8 ? 1 : 8 / WM, NT = WM == 1 ? 4 : 8;
-    static constexpr int GROUPS = WN * NT;               // operands of a row tile: 32, 32, 16, 8
+    static constexpr int WN = 8 / WM, NT = WM == 1 ? 4 : 8;
+    static constexpr int GROUPS = WN * NT;               // operands of a row tile: 32, 16, 8
     static constexpr int PARTS = 32 / GROUPS;            // workgroups that share a chunk
     static constexpr int TILES = 256 / GROUPS;           // row tiles in a buffer
     static constexpr int KS = TILES / 4;                 // steps of 64 rows in a buffer
@@ -511,7 +509,8 @@ constexpr int kGradCus = 256;
 static GradPlan grad_plan(const Layout &L, int batch)
 {
     GradPlan p;
-    p.wm = batch <= 16 ? 1 : (batch <= 32 ? 2 : (batch <= 64 ? 4 : 8));
+    // (two waves along the vectors, 17 to 32 of them, were slower than two workgroups with one: 8192 x 8192, 32 vectors 32.8 us, 30.7)
+    p.wm = batch <= 32 ? 1 : (batch <= 64 ? 4 : 8);
     p.blocks = L.cq * (p.wm == 8 ? 4 : (p.wm == 4 ? 2 : 1));
     p.ks = p.wm == 8 ? 8 : (p.wm == 4 ? 4 : 2);
     p.steps = (L.rt_count + 3) / 4;
@@ -538,8 +537,8 @@ size_t grad_workspace_bytes(const Layout &L, int batch) { return grad_plan(L, ba
 
 #define PB_GRAD(WM) {{reinterpret_cast<const void *>(k_grad<1, false, WM>), reinterpret_cast<const void *>(k_grad<1, true, WM>)}, \
                      {reinterpret_cast<const void *>(k_grad<2, false, WM>), reinterpret_cast<const void *>(k_grad<2, true, WM>)}}
-static const void *const kGradFn[4][2][2] = {PB_GRAD(1), PB_GRAD(2), PB_GRAD(4), PB_GRAD(8)};
-constexpr int kGradLds[4] = {GradShape<1>::LDS, GradShape<2>::LDS, GradShape<4>::LDS, GradShape<8>::LDS};
+static const void *const kGradFn[3][2][2] = {PB_GRAD(1), PB_GRAD(4), PB_GRAD(8)};
+constexpr int kGradLds[3] = {GradShape<1>::LDS, GradShape<4>::LDS, GradShape<8>::LDS};
 
 int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, int bits_used, const float *dY, const GatedSource *gated,
                 int batch, float *dX, void *workspace, hipStream_t st)
@@ -563,9 +562,7 @@ int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, in
     err = (int)hipGetLastError();
     if (err) return err;
     const int waves = own ? 16 : 4, may_narrow = p.wm >= 4;
-    const bool vec = (L.gate_h ? L.gate_h : L.rows) % 4 == 0;
-    hipLaunchKernelGGL(vec ? (own ? k_grad_digits<true, true> : k_grad_digits<true, false>)
-                           : (own ? k_grad_digits<false, true> : k_grad_digits<false, false>),
+    hipLaunchKernelGGL(own ? k_grad_digits<true> : k_grad_digits<false>,
                        dim3((unsigned)((p.steps + waves - 1) / waves), (unsigned)((batch + 15) / 16)), dim3((unsigned)waves * 64), 0, st, dY,
                        scalings, batch, L.rows, L.gate_h, p.steps, may_narrow, digits);
     err = (int)hipGetLastError();
@@ -582,9 +579,9 @@ int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, in
     a.workgroups = a.blocks * a.rows_of * p.splits;
     float *const parts = reinterpret_cast<float *>(ws + p.parts_off);
     a.out = p.splits > 1 ? parts : dX;
-    const int shape = p.wm == 8 ? 3 : p.wm / 2, wide = bits_used > 4, il = is_pairs(L.layout);
+    const int shape = p.wm == 8 ? 2 : p.wm / 4, wide = bits_used > 4, il = is_pairs(L.layout);
     const void *fn = kGradFn[shape][wide][il];
-    static bool declared[4][2][2];      // (more than the default 64 KB of LDS)
+    static bool declared[3][2][2];      // (more than the default 64 KB of LDS)
     hipError_t e = hipSuccess;
     if (!__atomic_load_n(&declared[shape][wide][il], __ATOMIC_RELAXED)) {
         e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kGradLds[shape]);
