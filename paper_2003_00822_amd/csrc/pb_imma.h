@@ -385,6 +385,8 @@ inline int tile_rows(const TileShape &t, int m, bool sums)
     return groups >= t.nt ? 1 : t.nt / groups;
 }
 int launch_imma_tile(int shape, const I8Args &a, int nd, bool il, hipStream_t st);
+// Whether it takes a gated block's act(g) u along (the other shapes' registers are full)
+inline bool gated_tile(int shape) { return shape == 0; }
 
 // The kernel for large batches of the gated block and the adapters (pb_batch.hip): its workgroups, its launch (`partial`: [batch][R], used where
 // there are several groups of bitlayers)

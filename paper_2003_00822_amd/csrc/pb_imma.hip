@@ -351,8 +351,8 @@ int launch_imma(const uint32_t *packed, const float *scales, const Layout &L, in
         if (e) return e;
     }
     if (shape >= 0) {
-        if (a.gate < 0) return launch_imma_tile(shape, a, nd, il, st);
-        // a gated block: the pre-activations through memory
+        if (a.gate < 0 || gated_tile(shape)) return launch_imma_tile(shape, a, nd, il, st);
+        // a gated block in another shape: the pre-activations through memory
         if (!a.Y) a.Y = ep.pre;
         const int e = launch_imma_tile(shape, a, nd, il, st);
         return e ? e : launch_gated(a.Y, L.rows / 2, ep.gate, batch, ep.h_out, st);
