@@ -12,6 +12,8 @@
 #include <hip/hip_fp16.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "pb_kernels.h"
 
 namespace pb {
@@ -39,19 +41,22 @@ __device__ __forceinline__ v4f load4(const f16 *p)
     const u32x2 w = *reinterpret_cast<const u32x2_at2 *>(p);
     return v4f{to_f32(f16{(uint16_t)w[0]}), to_f32(f16{(uint16_t)(w[0] >> 16)}), to_f32(f16{(uint16_t)w[1]}), to_f32(f16{(uint16_t)(w[1] >> 16)})};
 }
-// The values p[at .. at + 4) of `length`, 0 beyond the end
-template <typename T>
+// The values p[at .. at + 4).  Unless WHOLE some may lie behind the last of `length`: the last stands for them (ZERO: 0).  (No branch: a load in a
+// branch of its own is waited for there.)
+template <bool WHOLE, bool ZERO, typename T>
 __device__ __forceinline__ v4f load4_of(const T *p, int at, int length)
 {
-    v4f v = {0, 0, 0, 0};
-    if (at + 4 <= length) {
-        v = load4(p + at);
+    if constexpr (WHOLE) {
+        return load4(p + at);
     } else {
+        v4f v;
 #pragma unroll
-        for (int i = 0; i < 3; ++i)
-            if (at + i < length) v[i] = to_f32(p[at + i]);
+        for (int e = 0; e < 4; ++e) {
+            v[e] = to_f32(p[min(at + e, length - 1)]);
+            if (ZERO && at + e >= length) v[e] = 0.0f;
+        }
+        return v;
     }
-    return v;
 }
 __device__ __forceinline__ void store4_of(float *p, int at, int length, v4f v)
 {
@@ -63,6 +68,8 @@ __device__ __forceinline__ void store4_of(float *p, int at, int length, v4f v)
             if (at + i < length) p[at + i] = v[i];
     }
 }
+typedef std::integral_constant<bool, true> yes;
+typedef std::integral_constant<bool, false> no;
 __device__ __forceinline__ v4f mfma(float a, float b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 // ---- the order of the vectors ----
@@ -232,50 +239,71 @@ struct DownArgs {
     const void *M;            // A or B
     const float *scale;       // (t only)
     const float *V;           // [batch][length]
-    float *out;               // [slice][vector][16 ranks]: rank tile after rank tile, 16 values each
+    float *out;               // [vector][rank, a multiple of 16][parts of the sum]
     int length, rank, ranks, slices;
 };
-// Parts of the sum of a tile's products go to the waves of `slices` workgroups; a lane's result is four ranks of one vector.
+// Parts of the sum of a tile's products go to the waves of `slices` workgroups (a power of two up to 16); a lane's result is four ranks of one
+// vector.  It is kept as a part per slice, four at least; those that no slice fills are zero.
 //   TURNED: the summands are the rows of the matrix (B: [length][rank]), else its columns (A: [rank][length])
+// What a lane loads of ranks beyond the last is another's; they are set to zero in the end.
+constexpr int kMany = 32, kPartsOfMany = 8;       // of more than 32 vectors (an adapter may have them all) eight parts at most
+__host__ __device__ constexpr int down_parts(int slices) { return slices > 4 ? slices : 4; }
 constexpr int kDownWaves = 8;
 template <typename T, bool TURNED, int RT>
-__device__ __forceinline__ void adapter_down(const DownArgs &a, int rt0, v4f (*s_part)[RT][64])
+__device__ __forceinline__ void adapter_down(const DownArgs &a, int own, v4f (*s_part)[RT][64])
 {
-    const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Order::Tile it;
     if (!a.order.tile(blockIdx.x, lane, &it)) return;
     const T *const M = static_cast<const T *>(a.M) + (size_t)it.adapter * a.rank * a.length;
     const float *const x = a.V + (size_t)it.vector * a.length;
+    // (RT tiles that there are, also where this workgroup's own are fewer: all but the last are whole)
+    const int rt0 = min(own, a.ranks - RT), last = min((rt0 + RT - 1) * 16 + i, a.rank - 1);
+    const T *row[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) row[t] = M + (size_t)(t < RT - 1 ? (rt0 + t) * 16 + i : last) * a.length;
     v4f acc[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[t] = v4f{0, 0, 0, 0};
-    for (int c0 = (blockIdx.y * kDownWaves + wave) * 64; c0 < a.length; c0 += a.slices * kDownWaves * 64) {
-        v4f v[4], w[4][RT];
+    // 16 Q summands from c0 on
+    auto step = [&](int c0, auto whole, auto many) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        constexpr int Q = decltype(many)::value;
+        v4f v[Q], w[Q][RT];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = load4_of(x, c0 + 16 * q + 4 * kb, a.length);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < Q; ++q) {
             const int c = c0 + 16 * q + 4 * kb;
+            v[q] = load4_of<WHOLE, true>(x, c, a.length);
+            if constexpr (TURNED) {
 #pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                const int j = (rt0 + t) * 16 + i;
-                w[q][t] = v4f{0, 0, 0, 0};
-                if (j < a.rank) {
-                    if constexpr (TURNED) {
+                for (int e = 0; e < 4; ++e) {
+                    const T *const m = M + (size_t)(c0 + 16 * q + e) * a.rank;       // (the same in all lanes)
+                    const int r = WHOLE ? 4 * kb : min(4 * kb, a.length - 1 - (c0 + 16 * q + e));
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) w[q][t][e] = c + e < a.length ? to_f32(M[(size_t)(c + e) * a.rank + j]) : 0.0f;
-                    } else {
-                        w[q][t] = load4_of(M + (size_t)j * a.length, c, a.length);
+                    for (int t = 0; t < RT; ++t) {
+                        w[q][t][e] = to_f32(m[r * a.rank + (t < RT - 1 ? (rt0 + t) * 16 + i : last)]);
+                        if (!WHOLE && c + e >= a.length) w[q][t][e] = 0.0f;
                     }
                 }
+            } else {
+#pragma unroll
+                for (int t = 0; t < RT; ++t) w[q][t] = load4_of<WHOLE, true>(row[t], c, a.length);
             }
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < Q; ++q)
 #pragma unroll
             for (int t = 0; t < RT; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[t] = mfma(w[q][t][e], v[q][e], acc[t]);
+    };
+    for (int c0 = (blockIdx.y * kDownWaves + wave) * 64; c0 < a.length; c0 += a.slices * kDownWaves * 64) {
+        if (c0 + 64 <= a.length) {
+            step(c0, yes(), std::integral_constant<int, 4>());
+        } else {
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) step(c0 + 16 * q, no(), std::integral_constant<int, 1>());
+        }
     }
     if (wave > 0) {
 #pragma unroll
@@ -286,7 +314,7 @@ __device__ __forceinline__ void adapter_down(const DownArgs &a, int rt0, v4f (*s
     const float s = a.scale ? a.scale[it.adapter] : 1.0f;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        if (rt0 + t >= a.ranks) break;
+        if (rt0 + t < own) continue;
         v4f v = acc[t];
 #pragma unroll
         for (int w = 0; w < kDownWaves - 1; ++w) v += s_part[w][t][lane];
@@ -295,7 +323,14 @@ __device__ __forceinline__ void adapter_down(const DownArgs &a, int rt0, v4f (*s
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if ((rt0 + t) * 16 + 4 * kb + e >= a.rank) v[e] = 0.0f;
-        *reinterpret_cast<v4f *>(a.out + (((size_t)blockIdx.y * a.order.batch + it.vector) * a.ranks + rt0 + t) * 16 + 4 * kb) = v;
+        const int parts = down_parts(a.slices), own_parts = parts / a.slices;
+        float *const out = a.out + (((size_t)it.vector * a.ranks + rt0 + t) * 16 + 4 * kb) * parts + blockIdx.y * own_parts;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (own_parts == 4) *reinterpret_cast<v4f *>(out + e * parts) = v4f{v[e], 0, 0, 0};
+            else if (own_parts == 2) *reinterpret_cast<float2 *>(out + e * parts) = make_float2(v[e], 0.0f);
+            else out[e * parts] = v[e];
+        }
     }
 }
 // u, t or both
@@ -307,20 +342,23 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_adapter_down(const DownArgs
     if (u.V && z < u.ranks) adapter_down<T, false, RT>(u, z, s_part);
     else adapter_down<T, true, RT>(t, u.V ? z - (u.ranks + RT - 1) / RT * RT : z, s_part);
 }
-// Ranks 4 part .. 4 part + 3 of rank tile `rt` of a vector: the slices added up in their order
-__device__ __forceinline__ v4f down_at(const float *parts, int slices, int batch, int ranks, int vector, int rt, int part)
+// Rank i of rank tile `rt` of a vector: the parts added up in a fixed order
+template <int PARTS>
+__device__ __forceinline__ float down_at(const float *parts, int ranks, int vector, int rt, int i)
 {
-    const float *p = parts + ((size_t)vector * ranks + rt) * 16 + 4 * part;
-    v4f v = *reinterpret_cast<const v4f *>(p);
-    for (int s = 1; s < slices; ++s) v += *reinterpret_cast<const v4f *>(p + (size_t)s * batch * ranks * 16);
-    return v;
+    const v4f *const p = reinterpret_cast<const v4f *>(parts + (((size_t)vector * ranks + rt) * 16 + i) * PARTS);
+    v4f v = p[0];
+#pragma unroll
+    for (int k = 1; k < PARTS / 4; ++k) v += p[k];
+    return (v[0] + v[1]) + (v[2] + v[3]);
 }
-__device__ __forceinline__ float down1_at(const float *parts, int slices, int batch, int ranks, int vector, int rt, int i)
+// f(integral constant of the parts, MOST at most)
+template <int MOST, typename F>
+__device__ __forceinline__ void by_parts(int slices, F f)
 {
-    const float *p = parts + ((size_t)vector * ranks + rt) * 16 + i;
-    float v = *p;
-    for (int s = 1; s < slices; ++s) v += p[(size_t)s * batch * ranks * 16];
-    return v;
+    if (slices <= 4) f(std::integral_constant<int, 4>());
+    else if (slices == 8 || MOST == 8) f(std::integral_constant<int, 8>());
+    else f(std::integral_constant<int, MOST>());
 }
 
 // ---- Y += scale_k B_k u, dX += A_k^T t ----
@@ -332,16 +370,33 @@ struct UpArgs {
     float *out;               // [batch][length]
     int length, rank, ranks, slices, blocks;
 };
-// A wave does `blocks` times 64 values of the tile's vectors.  RT rank tiles at once.  TURNED: M is A [rank][length], else B [length][rank]
+// A wave does `blocks` times 64 values of the tile's vectors.  RT rank tiles at once.  TURNED: M is A [rank][length], else B [length][rank].
+// Values behind the last are computed from others' rows or columns and not stored.
+constexpr int kUpRow = 20;        // floats per rank in LDS: the vectors of the tile, and room that puts neighbouring ranks on other banks
 template <typename T, bool TURNED, int RT>
 __global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
 {
-    const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int first = (blockIdx.x * 4 + wave) * a.blocks * 64, end = min(first + a.blocks * 64, a.length);
+    __shared__ float s_u[PB_MAX_RANK * kUpRow];
     Order::Tile it;
-    if (first >= a.length || !a.order.tile(blockIdx.y, lane, &it)) return;
+    if (!a.order.tile(blockIdx.y, lane, &it)) return;
     const T *const M = static_cast<const T *>(a.M) + (size_t)it.adapter * a.rank * a.length;
     const float s = a.scale ? a.scale[it.adapter] : 1.0f;
+    // the parts of u (t) are added up once per workgroup: a thread has a rank of every rank tile of one vector
+    by_parts<16>(a.slices, [&](auto parts) {
+        const int v = threadIdx.x / 16, vector = __shfl(it.vector, v);
+        for (int rt0 = 0; rt0 < a.ranks; rt0 += RT) {
+            float sum[RT];
+#pragma unroll
+            for (int t = 0; t < RT; ++t) sum[t] = down_at<decltype(parts)::value>(a.parts, a.ranks, vector, min(rt0 + t, a.ranks - 1), i) * s;
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+                if (rt0 + t < a.ranks) s_u[((rt0 + t) * 16 + i) * kUpRow + v] = sum[t];
+        }
+    });
+    __syncthreads();
+    if (first >= a.length) return;
     float *const y = a.out + (size_t)it.vector * a.length;
     // a lane's values: four times four next to each other
     auto value_at = [&](int r0, int t) { return r0 + 16 * t + 4 * kb; };
@@ -349,33 +404,20 @@ __global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
     float u[RT][4];
     auto load_u = [&](int rt0) {
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            if (rt0 + t < a.ranks) {
-                if constexpr (TURNED) {
+        for (int t = 0; t < RT; ++t)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) u[t][e] = down1_at(a.parts, a.slices, a.order.batch, a.ranks, it.vector, rt0 + t, 4 * e + kb);
-                } else {
-                    const v4f v = down_at(a.parts, a.slices, a.order.batch, a.ranks, it.vector, rt0 + t, kb) * s;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) u[t][e] = v[e];
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) u[t][e] = 0.0f;
-            }
-        }
+            for (int e = 0; e < 4; ++e)
+                u[t][e] = rt0 + t < a.ranks ? s_u[((rt0 + t) * 16 + (TURNED ? 4 * e + kb : 4 * kb + e)) * kUpRow + i] : 0.0f;
     };
-    v4f before[4];
-    auto load_before = [&](int r0) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) before[t] = load4_of(y, value_at(r0, t), end);
-    };
-    load_before(first);
     load_u(0);
-    for (int r0 = first; r0 < end; r0 += 64) {
-        v4f acc[4];
+    auto block = [&](int r0, auto whole, auto fours) {
+        constexpr bool WHOLE = decltype(whole)::value, FOURS = decltype(fours)::value;
+        v4f before[4], acc[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) acc[t] = v4f{0, 0, 0, 0};
+        for (int t = 0; t < 4; ++t) {
+            before[t] = load4_of<WHOLE, false>(y, value_at(r0, t), a.length);
+            acc[t] = v4f{0, 0, 0, 0};
+        }
         for (int rt0 = 0; rt0 < a.ranks; rt0 += RT) {
             if (a.ranks > RT) load_u(rt0);
             v4f w[RT][4];
@@ -383,14 +425,20 @@ __global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
             for (int x = 0; x < RT; ++x)
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    w[x][t] = v4f{0, 0, 0, 0};
+                    bool inside;
                     if constexpr (TURNED) {      // t: summand 4 t + kb, four values (in the order in which a lane's results then are four and four)
                         const int j = (rt0 + x) * 16 + 4 * t + kb;
-                        if (j < a.rank) w[x][t] = load4_of(M + (size_t)j * a.length, r0 + 16 * (i & 3) + 4 * (i >> 2), a.length);
+                        inside = j < a.rank;
+                        w[x][t] = load4_of<WHOLE, false>(M + (size_t)min(j, a.rank - 1) * a.length, r0 + 16 * (i & 3) + 4 * (i >> 2), a.length);
                     } else {                     // t: value r0 + 16 t + i, the summands 4 kb .. 4 kb + 3
-                        const int r = r0 + 16 * t + i;
-                        if (r < a.length) w[x][t] = load4_of(M + (size_t)r * a.rank, (rt0 + x) * 16 + 4 * kb, a.rank);
+                        const int j = (rt0 + x) * 16 + 4 * kb;
+                        const T *const row = M + (size_t)(WHOLE ? r0 + 16 * t + i : min(r0 + 16 * t + i, a.length - 1)) * a.rank;
+                        inside = !FOURS || j < a.rank;
+                        w[x][t] = load4_of<FOURS, true>(row, FOURS ? min(j, a.rank - 4) : j, a.rank);
                     }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!inside) w[x][t][e] = 0.0f;
                 }
 #pragma unroll
             for (int x = 0; x < RT; ++x)
@@ -402,17 +450,25 @@ __global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
                         else acc[t] = mfma(w[x][t][e], u[x][e], acc[t]);
                     }
         }
-        v4f now[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) now[t] = before[t];
-        if (r0 + 64 < end) load_before(r0 + 64);
         if (i < it.length) {
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 v4f v = acc[t];
                 if constexpr (TURNED) v = v4f{acc[0][t], acc[1][t], acc[2][t], acc[3][t]};
-                store4_of(y, value_at(r0, t), end, now[t] + v);
+                v += before[t];
+                if constexpr (WHOLE) *reinterpret_cast<v4f_at4 *>(y + value_at(r0, t)) = v;
+                else store4_of(y, value_at(r0, t), a.length, v);
             }
+        }
+    };
+    // (B's rows in fours where the rank is a multiple of four: every lane's four are ranks, or none is)
+    const bool fours = TURNED || a.rank % 4 == 0;
+    for (int r0 = first; r0 < end; r0 += 64) {
+        if (r0 + 64 <= a.length) {
+            if (fours) block(r0, yes(), yes());
+            else block(r0, yes(), no());
+        } else {
+            block(r0, no(), no());
         }
     }
 }
@@ -426,13 +482,17 @@ struct OuterArgs {
     float *out;               // TURNED: [adapter][length][rank], else [adapter][rank][length]
     int length, rank, ranks, slices;
 };
-constexpr int kOuterWaves = 8;
-// A workgroup does 64 columns (rows) and RT rank tiles of an adapter; its waves take every eighth four of the adapter's vectors.
-template <bool TURNED, int RT>
-__device__ __forceinline__ void adapter_outer(const OuterArgs &a, int block, v4f (*s_part)[RT * 4][64])
+// A wave does 64 columns (rows) and RT rank tiles of an adapter.  SPLIT: the waves of a workgroup do the same ones and take the adapter's vectors by
+// fours in turn, and their sums meet in LDS, where every wave adds up a part; else each has columns of its own, and u (t) comes from LDS.
+constexpr int outer_waves(bool split) { return split ? 16 : 4; }
+constexpr int kOuterVectors = 8;       // (not split) vectors whose ranks are in LDS at a time
+constexpr int outer_lds(bool split, int rt) { return split ? outer_waves(true) * rt * 4 * 64 * 4 : rt * 16 * kOuterVectors; }      // in floats
+template <bool TURNED, bool SPLIT, int RT>
+__device__ __forceinline__ void adapter_outer(const OuterArgs &a, int block, float *lds)
 {
-    const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
-    const int k = blockIdx.y, rt0 = blockIdx.z * RT, c = block * 64 + 4 * i;
+    constexpr int WAVES = SPLIT ? outer_waves(true) : 1;
+    const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int k = blockIdx.y, rt0 = blockIdx.z * RT, c0 = (SPLIT ? block : block * outer_waves(false) + wave) * 64, c = c0 + 4 * i;
     const Order::Segment seg = a.order.segment(k, lane);
     v4f acc[RT][4];
 #pragma unroll
@@ -440,70 +500,101 @@ __device__ __forceinline__ void adapter_outer(const OuterArgs &a, int block, v4f
 #pragma unroll
         for (int q = 0; q < 4; ++q) acc[t][q] = v4f{0, 0, 0, 0};
     // (several requests of vectors at once: their numbers first, then what depends on them)
-    constexpr int AT_ONCE = RT == 1 ? 8 : 4;
-    for (int p0 = 4 * wave; p0 < seg.length; p0 += AT_ONCE * 4 * kOuterWaves) {
-        int n[AT_ONCE];
-        v4f v[AT_ONCE];
-        float u[AT_ONCE][RT];
+    constexpr int AT_ONCE = SPLIT ? 4 : kOuterVectors / 4;
+    auto sums = [&](auto whole, auto parts) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        constexpr int PARTS = decltype(parts)::value;
+        for (int p0 = SPLIT ? 4 * wave : 0; p0 < seg.length; p0 += AT_ONCE * 4 * WAVES) {
+            int n[AT_ONCE];
+            v4f v[AT_ONCE];
+            float u[AT_ONCE][RT];
 #pragma unroll
-        for (int x = 0; x < AT_ONCE; ++x) {
-            const int p = p0 + x * 4 * kOuterWaves + kb;
-            n[x] = seg.vector(min(p, seg.length - 1));
-            if (p >= seg.length) n[x] = -1;
+            for (int x = 0; x < AT_ONCE; ++x) n[x] = seg.vector(min(p0 + x * 4 * WAVES + kb, seg.length - 1));
+#pragma unroll
+            for (int x = 0; x < AT_ONCE; ++x) v[x] = load4_of<WHOLE, false>(a.V + (size_t)n[x] * a.length, c, a.length);
+            if constexpr (SPLIT) {
+#pragma unroll
+                for (int x = 0; x < AT_ONCE; ++x)
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) u[x][t] = down_at<PARTS>(a.parts, a.ranks, n[x], min(rt0 + t, a.ranks - 1), i);
+            } else {
+                // a thread brings rank i of one vector and of every second rank tile
+                const int m = threadIdx.x / 16 % kOuterVectors, t0 = threadIdx.x / (16 * kOuterVectors), of = seg.vector(min(p0 + m, seg.length - 1));
+                float sum[(RT + 1) / 2];
+#pragma unroll
+                for (int y = 0; y < (RT + 1) / 2; ++y) sum[y] = down_at<PARTS>(a.parts, a.ranks, of, min(rt0 + t0 + 2 * y, a.ranks - 1), i);
+                __syncthreads();
+#pragma unroll
+                for (int y = 0; y < (RT + 1) / 2; ++y)
+                    if (t0 + 2 * y < RT) lds[((t0 + 2 * y) * kOuterVectors + m) * 16 + i] = sum[y];
+                __syncthreads();
+#pragma unroll
+                for (int x = 0; x < AT_ONCE; ++x)
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) u[x][t] = lds[(t * kOuterVectors + 4 * x + kb) * 16 + i];
+            }
+#pragma unroll
+            for (int x = 0; x < AT_ONCE; ++x) {
+                if (p0 + x * 4 * WAVES + kb >= seg.length) {      // (a vector that was loaded in place of one behind the last)
+                    v[x] = v4f{0, 0, 0, 0};
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) u[x][t] = 0.0f;
+                }
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[t][q] = mfma(u[x][t], v[x][q], acc[t][q]);
+            }
         }
-#pragma unroll
-        for (int x = 0; x < AT_ONCE; ++x) {
-            v[x] = n[x] >= 0 ? load4_of(a.V + (size_t)n[x] * a.length, c, a.length) : v4f{0, 0, 0, 0};
-#pragma unroll
-            for (int t = 0; t < RT; ++t)
-                u[x][t] = n[x] >= 0 && rt0 + t < a.ranks ? down1_at(a.parts, a.slices, a.order.batch, a.ranks, n[x], rt0 + t, i) : 0.0f;
+    };
+    // (the same in all waves of a workgroup, which meet at barriers)
+    const bool whole = (SPLIT ? c0 + 64 : (block + 1) * outer_waves(false) * 64) <= a.length;
+    by_parts<SPLIT ? kPartsOfMany : 16>(a.slices, [&](auto parts) {
+        if (whole) sums(yes(), parts);
+        else sums(no(), parts);
+    });
+    const float s = a.scale ? a.scale[k] : 1.0f;
+    // Part x of rank tile t, four values next to each other in memory: of column c + x the ranks j .. j + 3 (TURNED), of rank j + x the columns c .. c + 3
+    auto part = [&](int t, int x) {
+        if constexpr (TURNED) return acc[t][x];
+        else return v4f{acc[t][0][x], acc[t][1][x], acc[t][2][x], acc[t][3][x]};
+    };
+    auto store = [&](int t, int x, v4f v) {
+        const int j = (rt0 + t) * 16 + 4 * kb;
+        if constexpr (TURNED) {
+            if (c + x < a.length) store4_of(a.out + ((size_t)k * a.length + c + x) * a.rank, j, a.rank, v * s);
+        } else {
+            if (j + x < a.rank) store4_of(a.out + ((size_t)k * a.rank + j + x) * a.length, c, a.length, v * s);
         }
-#pragma unroll
-        for (int x = 0; x < AT_ONCE; ++x)
-#pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) acc[t][q] = mfma(u[x][t], v[x][q], acc[t][q]);
-    }
-    if (wave > 0) {
+    };
+    if constexpr (SPLIT) {
+        v4f *const s_part = reinterpret_cast<v4f *>(lds);
 #pragma unroll
         for (int t = 0; t < RT; ++t)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) s_part[wave - 1][t * 4 + q][lane] = acc[t][q];
-    }
-    __syncthreads();
-    if (wave > 0) return;
-    const float s = a.scale ? a.scale[k] : 1.0f;
+            for (int x = 0; x < 4; ++x) s_part[(wave * RT * 4 + t * 4 + x) * 64 + lane] = part(t, x);
+        __syncthreads();
+        if (wave >= RT * 4) return;
+        v4f v = {0, 0, 0, 0};
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
+        for (int w = 0; w < WAVES; ++w) v += s_part[(w * RT * 4 + wave) * 64 + lane];
+        store(wave / 4, wave % 4, v);
+    } else {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            for (int w = 0; w < kOuterWaves - 1; ++w) acc[t][q] += s_part[w][t * 4 + q][lane];
-            acc[t][q] *= s;
-        }
-        // the lane has ranks j .. j + 3 of the columns c .. c + 3
-        const int j = (rt0 + t) * 16 + 4 * kb;
-        if constexpr (TURNED) {
+        for (int t = 0; t < RT; ++t)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (c + q < a.length) store4_of(a.out + ((size_t)k * a.length + c + q) * a.rank, j, a.rank, acc[t][q]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (j + e < a.rank)
-                    store4_of(a.out + ((size_t)k * a.rank + j + e) * a.length, c, a.length, v4f{acc[t][0][e], acc[t][1][e], acc[t][2][e], acc[t][3][e]});
-        }
+            for (int x = 0; x < 4; ++x) store(t, x, part(t, x));
     }
 }
 
 // dA, dB or both
-template <int RT>
-__global__ __launch_bounds__(kOuterWaves * 64) void k_adapter_outer(const OuterArgs A, const OuterArgs B)
+template <bool SPLIT, int RT>
+__global__ __launch_bounds__(outer_waves(SPLIT) * 64) void k_adapter_outer(const OuterArgs A, const OuterArgs B, const int of_A)
 {
-    __shared__ v4f s_part[kOuterWaves - 1][RT * 4][64];
-    const int block = blockIdx.x, of_A = A.out ? (A.length + 63) / 64 : 0;
-    if (block < of_A) adapter_outer<false, RT>(A, block, s_part);
-    else adapter_outer<true, RT>(B, block - of_A, s_part);
+    __shared__ __align__(16) float lds[outer_lds(SPLIT, RT)];
+    const int block = blockIdx.x;
+    if (block < of_A) adapter_outer<false, SPLIT, RT>(A, block, lds);
+    else adapter_outer<true, SPLIT, RT>(B, block - of_A, lds);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -514,13 +605,13 @@ AdapterPlan adapter_plan(const Layout &L, const pb_adapters &ad, int batch, bool
     const int tiles = (batch + 15) / 16;
     p.items = indexed ? (ad.count + batch / 16 < batch ? ad.count + batch / 16 : batch) : tiles;
     p.ranks = (ad.rank + 15) / 16;
-    // parts of the sums: about two workgroups per compute unit, each wave with 64 summands or more
-    const int most = L.rows > L.cols ? L.rows : L.cols;
-    int slices = 512 / (p.items * ((p.ranks + 3) / 4));
-    if (slices > (most + 64 * kDownWaves - 1) / (64 * kDownWaves)) slices = (most + 64 * kDownWaves - 1) / (64 * kDownWaves);
-    p.slices = slices < 1 ? 1 : (slices > 16 ? 16 : slices);
+    // parts of the sums: about two workgroups per compute unit (one does not get more than its share of the memory's rate by much), each wave with
+    // 64 summands or more
+    const int most = L.rows > L.cols ? L.rows : L.cols, z = (p.ranks + 3) / 4;
+    p.slices = 1;
+    while (p.slices < (batch > kMany ? kPartsOfMany : 16) && p.items * z * p.slices < 384 && p.slices * 64 * kDownWaves < most) p.slices *= 2;
     auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
-    const size_t down = up((size_t)p.slices * batch * p.ranks * 64);
+    const size_t down = up((size_t)batch * p.ranks * 64 * down_parts(p.slices));
     p.items_off = up((size_t)batch * 4);
     p.counts_off = up(p.items_off + (size_t)p.items * sizeof(Item));
     p.starts_off = p.counts_off + 256;
@@ -553,6 +644,12 @@ int launch_adapter_order(const AdapterPlan &p, const pb_adapters &ad, const int3
     return (int)hipGetLastError();
 }
 
+// Rank tiles that a wave takes at once, four at most and no more than it needs
+static int rank_tiles(int ranks)
+{
+    const int turns = (ranks + 3) / 4;
+    return (ranks + turns - 1) / turns;
+}
 // fn(T(), ...) for the type of the adapters
 template <typename F>
 static int by_type(int type, F fn)
@@ -569,9 +666,9 @@ static int launch(const void *fn, dim3 grid, int threads, void *args, hipStream_
     const hipError_t e = hipLaunchKernel(fn, grid, dim3((unsigned)threads), list, 0, st);
     return (int)(e != hipSuccess ? e : hipGetLastError());
 }
-static int launch_two(const void *fn, dim3 grid, int threads, void *first, void *second, hipStream_t st)
+static int launch(const void *fn, dim3 grid, int threads, void *first, void *second, void *third, hipStream_t st)
 {
-    void *list[] = {first, second};
+    void *list[] = {first, second, third};
     const hipError_t e = hipLaunchKernel(fn, grid, dim3((unsigned)threads), list, 0, st);
     return (int)(e != hipSuccess ? e : hipGetLastError());
 }
@@ -580,7 +677,7 @@ int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layou
                         void *workspace, hipStream_t st)
 {
     char *const ws = static_cast<char *>(workspace);
-    const int rt = p.ranks >= 3 ? 4 : p.ranks, z = (p.ranks + rt - 1) / rt;
+    const int rt = rank_tiles(p.ranks), z = (p.ranks + rt - 1) / rt;
     DownArgs u, t;
     u.order = order_of(p, ad, index, batch, workspace);
     u.rank = ad.rank; u.ranks = p.ranks; u.slices = p.slices;
@@ -589,9 +686,10 @@ int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layou
     t.M = ad.B; t.scale = ad.scale; t.V = dY; t.length = L.rows; t.out = reinterpret_cast<float *>(ws + p.t_off);
     return by_type(ad.type, [&](auto type) {
         typedef decltype(type) T;
-        const void *fn = rt == 1 ? reinterpret_cast<const void *>(k_adapter_down<T, 1>)
-                                 : (rt == 2 ? reinterpret_cast<const void *>(k_adapter_down<T, 2>) : reinterpret_cast<const void *>(k_adapter_down<T, 4>));
-        return launch_two(fn, dim3((unsigned)p.items, (unsigned)p.slices, (unsigned)(z * ((X ? 1 : 0) + (dY ? 1 : 0)))), kDownWaves * 64, &u, &t, st);
+        static const void *const fn[4] = {reinterpret_cast<const void *>(k_adapter_down<T, 1>), reinterpret_cast<const void *>(k_adapter_down<T, 2>),
+                                          reinterpret_cast<const void *>(k_adapter_down<T, 3>), reinterpret_cast<const void *>(k_adapter_down<T, 4>)};
+        return launch(fn[rt - 1], dim3((unsigned)p.items, (unsigned)p.slices, (unsigned)(z * ((X ? 1 : 0) + (dY ? 1 : 0)))), kDownWaves * 64, &u, &t,
+                      nullptr, st);
     });
 }
 
@@ -611,12 +709,12 @@ static int launch_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &
     // Blocks of 64 values per wave: one while that leaves the chip room, up to four (a wave finds its tile and its ranks once)
     const long long waves = (long long)((a.length + 63) / 64) * p.items;
     a.blocks = waves < 2 * 4096 ? 1 : (waves < 4 * 4096 ? 2 : 4);
-    const int rt = p.ranks >= 3 ? 4 : p.ranks;
+    const int rt = rank_tiles(p.ranks);
     return by_type(ad.type, [&](auto type) {
         typedef decltype(type) T;
-        const void *fn = rt == 1 ? reinterpret_cast<const void *>(k_adapter_up<T, TURNED, 1>)
-                                 : (rt == 2 ? reinterpret_cast<const void *>(k_adapter_up<T, TURNED, 2>) : reinterpret_cast<const void *>(k_adapter_up<T, TURNED, 4>));
-        return launch(fn, dim3((unsigned)((a.length + 256 * a.blocks - 1) / (256 * a.blocks)), (unsigned)p.items), 256, &a, st);
+        static const void *const fn[4] = {reinterpret_cast<const void *>(k_adapter_up<T, TURNED, 1>), reinterpret_cast<const void *>(k_adapter_up<T, TURNED, 2>),
+                                          reinterpret_cast<const void *>(k_adapter_up<T, TURNED, 3>), reinterpret_cast<const void *>(k_adapter_up<T, TURNED, 4>)};
+        return launch(fn[rt - 1], dim3((unsigned)((a.length + 256 * a.blocks - 1) / (256 * a.blocks)), (unsigned)p.items), 256, &a, st);
     });
 }
 
@@ -641,10 +739,16 @@ int launch_adapter_grads(const AdapterPlan &p, const pb_adapters &ad, const Layo
     B = A;
     A.scale = nullptr; A.parts = reinterpret_cast<const float *>(ws + p.t_off); A.V = X; A.out = dA; A.length = L.cols;
     B.scale = ad.scale; B.parts = reinterpret_cast<const float *>(ws + p.u_off); B.V = dY; B.out = dB; B.length = L.rows;
-    const int rt = p.ranks == 1 ? 1 : 2;
-    const void *fn = rt == 1 ? reinterpret_cast<const void *>(k_adapter_outer<1>) : reinterpret_cast<const void *>(k_adapter_outer<2>);
-    const int blocks = (dA ? (L.cols + 63) / 64 : 0) + (dB ? (L.rows + 63) / 64 : 0);
-    return launch_two(fn, dim3((unsigned)blocks, (unsigned)ad.count, (unsigned)((p.ranks + rt - 1) / rt)), kOuterWaves * 64, &A, &B, st);
+    // Adapters of many vectors are split over the waves along those (by the mean: where the vectors' adapters are is known on the device only)
+    const bool split = batch > kMany * ad.count;
+    const int rt = split ? (p.ranks == 1 ? 1 : 2) : rank_tiles(p.ranks), columns = split ? 64 : 64 * outer_waves(false);
+    static const void *const fns[2][4] = {{reinterpret_cast<const void *>(k_adapter_outer<false, 1>), reinterpret_cast<const void *>(k_adapter_outer<false, 2>),
+                                           reinterpret_cast<const void *>(k_adapter_outer<false, 3>), reinterpret_cast<const void *>(k_adapter_outer<false, 4>)},
+                                          {reinterpret_cast<const void *>(k_adapter_outer<true, 1>), reinterpret_cast<const void *>(k_adapter_outer<true, 2>)}};
+    int of_A = dA ? (L.cols + columns - 1) / columns : 0;
+    const int of_B = dB ? (L.rows + columns - 1) / columns : 0;
+    return launch(fns[split][rt - 1], dim3((unsigned)(of_A + of_B), (unsigned)ad.count, (unsigned)((p.ranks + rt - 1) / rt)), outer_waves(split) * 64, &A,
+                  &B, &of_A, st);
 }
 
 }  // namespace pb
