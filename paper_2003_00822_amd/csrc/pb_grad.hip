@@ -136,6 +136,53 @@ __global__ __launch_bounds__(1024) void k_gated_grad(const float *__restrict__ p
 // Whether one of the group's vectors needs four digits; the lane's vector is the group's vector lane % 16
 __device__ __forceinline__ bool group_is_wide(const Scaling &mine, bool live) { return __builtin_amdgcn_ballot_w64(live && mine.wide) != 0; }
 
+// The values of the sixteen packed rows of row tile 4 step + lane / 16, zero behind the last row.  (Four rows of the tile are next to each other in the
+// matrix; on the gate layout the units 4 t .. 4 t + 3 of a gate, rows 4 (unit) + gate of tile t.)  No branch per lane: a load in one is waited for there.
+__device__ __forceinline__ void rows_of_step(const float *y, int step, int lane, int rows, int gate_h, float (&v)[16])
+{
+    const int tile = step * 4 + (lane >> 4), height = gate_h ? gate_h : rows, first = gate_h ? tile * 4 : tile * kTileRows;
+    auto load = [&](auto whole) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int r = gate_h ? first : first + 4 * k;
+            const float *const at = y + (gate_h ? (size_t)k * gate_h : 0);
+            float4_at4 x;
+            if constexpr (decltype(whole)::value) {
+                x = *reinterpret_cast<const float4_at4 *>(at + r);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[i] = at[min(r + i, height - 1)];
+                    if (r + i >= height) x[i] = 0.0f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (gate_h) v[4 * i + k] = x[i];
+                else v[4 * k + i] = x[i];
+            }
+        }
+    };
+    if ((step * 4 + 4) * (gate_h ? 4 : kTileRows) <= height) load(std::integral_constant<bool, true>());
+    else load(std::integral_constant<bool, false>());
+}
+// Their digits, rint(v 2^e): the sixteen bytes of each
+__device__ __forceinline__ void digits_of(const float (&v)[16], int e, int balance, u32x4 (&out)[4])
+{
+    int g[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) g[i] = e == kNotFinite ? 0 : (__float2int_rn(ldexpf(v[i], e)) + balance) ^ balance;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const uint32_t a = __builtin_amdgcn_perm(g[4 * r + 1], g[4 * r], 0x05010400u), b = __builtin_amdgcn_perm(g[4 * r + 3], g[4 * r + 2], 0x05010400u);
+        const uint32_t c = __builtin_amdgcn_perm(g[4 * r + 1], g[4 * r], 0x07030602u), d = __builtin_amdgcn_perm(g[4 * r + 3], g[4 * r + 2], 0x07030602u);
+        out[0][r] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+        out[1][r] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        out[2][r] = __builtin_amdgcn_perm(d, c, 0x05040100u);
+        out[3][r] = __builtin_amdgcn_perm(d, c, 0x07060302u);
+    }
+}
+
 // The digits in memory: [group of 16 vectors][step of 64 packed rows][digit][lane 16 kb + v][16 bytes], the bytes being the
 // sixteen rows of row tile 4 step + kb of vector v: an operand of a digit of sixteen vectors is 1 KB in one piece.  A wave writes one step.
 // SCALES: every workgroup works the scalings of its sixteen vectors out by itself, a wave each, and the first of them leaves them in memory (a launch
@@ -144,8 +191,8 @@ template <bool SCALES>
 __global__ __launch_bounds__(SCALES ? 1024 : 256) void k_grad_digits(const float *__restrict__ dY, Scaling *__restrict__ scalings, int batch, int rows,
                                                                      int gate_h, int steps, int may_narrow, uint8_t *__restrict__ digits)
 {
-    const int lane = threadIdx.x & 63, step = blockIdx.x * (SCALES ? 16 : 4) + (threadIdx.x >> 6), group = blockIdx.y;
-    const int n = group * kGroupVectors + (lane & 15), tile = step * 4 + (lane >> 4);
+    const int lane = threadIdx.x & 63, step = blockIdx.x * (SCALES ? 16 : 4) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = blockIdx.y, n = group * kGroupVectors + (lane & 15);
     Scaling sc = {kNotFinite, kNotFinite, 0, 0};
     if constexpr (SCALES) {
         __shared__ Scaling s_scalings[kGroupVectors];
@@ -169,42 +216,10 @@ __global__ __launch_bounds__(SCALES ? 1024 : 256) void k_grad_digits(const float
     if (step >= steps) return;
     const bool narrow = may_narrow && !group_is_wide(sc, n < batch);
     const int e = narrow ? sc.e3 : sc.e4;
-    const float *const y = dY + (size_t)n * rows;
-    // (four rows of the tile are next to each other in the matrix; on the gate layout the units 4 t .. 4 t + 3 of a gate, rows 4 (unit) + gate of tile t)
     float v[16];
-    const int height = gate_h ? gate_h : rows;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int r = gate_h ? tile * 4 : tile * kTileRows + 4 * k;
-        const float *const at = y + (gate_h ? (size_t)k * gate_h : 0) + r;
-        float4_at4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (e != kNotFinite && r + 4 <= height) {
-            x = *reinterpret_cast<const float4_at4 *>(at);
-        } else if (e != kNotFinite) {
-#pragma unroll
-            for (int i = 0; i < 3; ++i)
-                if (r + i < height) x[i] = at[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (gate_h) v[4 * i + k] = x[i];
-            else v[4 * k + i] = x[i];
-        }
-    }
-    const int balance = narrow ? 0x8080 : 0x808080;
-    int g[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) g[i] = e == kNotFinite ? 0 : (__float2int_rn(ldexpf(v[i], e)) + balance) ^ balance;
+    rows_of_step(dY + (size_t)min(n, batch - 1) * rows, step, lane, rows, gate_h, v);
     u32x4 out[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const uint32_t a = __builtin_amdgcn_perm(g[4 * r + 1], g[4 * r], 0x05010400u), b = __builtin_amdgcn_perm(g[4 * r + 3], g[4 * r + 2], 0x05010400u);
-        const uint32_t c = __builtin_amdgcn_perm(g[4 * r + 1], g[4 * r], 0x07030602u), d = __builtin_amdgcn_perm(g[4 * r + 3], g[4 * r + 2], 0x07030602u);
-        out[0][r] = __builtin_amdgcn_perm(b, a, 0x05040100u);
-        out[1][r] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-        out[2][r] = __builtin_amdgcn_perm(d, c, 0x05040100u);
-        out[3][r] = __builtin_amdgcn_perm(d, c, 0x07060302u);
-    }
+    digits_of(v, e, narrow ? 0x8080 : 0x808080, out);
     u32x4 *dst = reinterpret_cast<u32x4 *>(digits + ((size_t)group * steps + step) * 4096) + lane;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -221,6 +236,8 @@ struct GradArgs {
     const Scaling *scalings;
     int may_narrow;
     float *out;                                      // [split][batch][cols]
+    const float *dY;                                 // (FUSED)
+    int rows, gate_h, held;                          // held: vectors in LDS, 4, 8 or 16
     int blocks, rows_of, workgroups;                 // column blocks, groups of vectors
 
     // What workgroup `id` does.  Workgroups go round the eight XCDs, each with an L2 of its own: those of an XCD (id % 8) take a contiguous range of an
@@ -253,13 +270,19 @@ struct GradShape {
 
 // While a wave multiplies the codes of one buffer, it turns its share of the words of the next one into codes: four words of each bitlayer per
 // lane, loaded with 16 bytes each (the vector-memory pipeline takes 16 cycles for a wave's load whatever its width).
-template <int Q, bool IL, int WM>
+// FUSED: the workgroup scales the gradients of its rows by their own largest and keeps their digits in LDS, behind the codes.
+constexpr int kFusedSteps = 28;           // of four vectors; of eight half of them, of sixteen a quarter
+constexpr int kFusedLds = kFusedSteps * 1024;
+template <int Q, bool IL, int WM, bool FUSED>
 __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
 {
+    static_assert(!FUSED || WM == 1);
     using S = GradShape<WM>;
     constexpr int WN = S::WN, NT = S::NT, TILES = S::TILES, KS = S::KS, TILE = S::TILE, BUF = TILES * TILE;
     extern __shared__ __align__(16) unsigned char s_codes[];
     __shared__ float s_scales[PB_MAX_BITS];
+    __shared__ uint32_t s_most[FUSED ? 8 : 1][16];
+    __shared__ int s_exponents[16];
 
     const int lane = threadIdx.x & 63, kb = lane >> 4, j = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -271,6 +294,11 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
     const int step0 = split * a.steps_per_split, step1 = min(step0 + a.steps_per_split, a.steps);   // (not empty)
     const int loops = (step1 - step0 + KS - 1) / KS;
     const int m = a.m;
+
+    // (FUSED) the values of the wave's first step, which stay in registers
+    const float *const y = FUSED ? a.dY + (size_t)min(group * kGroupVectors + j, a.batch - 1) * a.rows : nullptr;
+    float held[16];
+    if constexpr (FUSED) rows_of_step(y, min(step0 + wave, step1 - 1), lane, a.rows, a.gate_h, held);
 
     // the scales: whether they halve (as in k_i8_tile)
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.scales), 0, m * 4, 0x00020000);
@@ -289,7 +317,39 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
     // the digits of the wave's vectors in these steps (nothing beyond them, and nothing for a group without vectors)
     const __amdgpu_buffer_rsrc_t rd = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<uint8_t *>(a.digits) + ((size_t)group * a.steps + step0) * 4096, 0,
-        group * kGroupVectors < a.batch ? (step1 - step0) * 4096 : 0, 0x00020000);
+        !FUSED && group * kGroupVectors < a.batch ? (step1 - step0) * 4096 : 0, 0x00020000);
+    unsigned char *const s_digits = s_codes + S::LDS;      // [step][digit][kb][vector][16 bytes]
+    // the digits of the workgroup's rows: a wave has every eighth step (those behind its first are read again)
+    auto convert = [&] {
+        float v[16];
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) most = max(most, __float_as_uint(held[i]) & 0x7FFFFFFFu);
+#pragma unroll 1
+        for (int s = step0 + wave + 8; s < step1; s += 8) {
+            rows_of_step(y, s, lane, a.rows, a.gate_h, v);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+        }
+        most = max(most, (uint32_t)__shfl_xor((int)most, 16));
+        most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+        if (lane < 16) s_most[wave][lane] = most;
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < 8; ++x) most = max(most, s_most[x][j]);
+        const int e = scaling_of(most, 0.0, 0).e4;
+        if (threadIdx.x < 16) s_exponents[threadIdx.x] = e;
+#pragma unroll 1
+        for (int s = wave; s < step1 - step0; s += 8) {
+            if (s >= 8) rows_of_step(y, step0 + s, lane, a.rows, a.gate_h, held);
+            u32x4 out[4];
+            digits_of(held, e, 0x808080, out);
+            if (j < a.held) {
+#pragma unroll
+                for (int d = 0; d < 4; ++d) *reinterpret_cast<u32x4 *>(s_digits + (((s * 4 + d) * 4 + kb) * a.held + j) * 16) = out[d];
+            }
+        }
+    };
     // where the wave's operands begin in a buffer
     const unsigned char *const operands = s_codes + kb * TILE + wn * NT * 256 + j * 8;
 
@@ -373,10 +433,19 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
             u32x4 ar[2][DC];
             auto load_digits = [&](u32x4 (&dst)[DC], int step, int from) {
 #pragma unroll
-                for (int d = 0; d < DC; ++d) dst[d] = __builtin_amdgcn_raw_buffer_load_b128(rd, lane * 16, step * 4096 + (from + d) * 1024, 0);
+                for (int d = 0; d < DC; ++d) {
+                    if constexpr (FUSED)      // (lanes and steps beyond have others' digits: their vectors are not stored, their codes are zero)
+                        dst[d] = *reinterpret_cast<const u32x4 *>(s_digits + ((min(step, step1 - step0 - 1) * 4 + from + d) * 4 + kb) * a.held * 16 + min(j, a.held - 1) * 16);
+                    else
+                        dst[d] = __builtin_amdgcn_raw_buffer_load_b128(rd, lane * 16, step * 4096 + (from + d) * 1024, 0);
+                }
             };
             issue(0);
-            load_digits(ar[0], 0, 0);
+            if constexpr (FUSED) {
+                if (f == 0) convert();
+            } else {
+                load_digits(ar[0], 0, 0);
+            }
 #pragma unroll
             for (int i = 0; i < STAGES; ++i) {
                 expand(i, 0, my_codes);
@@ -384,6 +453,7 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
             }
             issue(1);
             __syncthreads();
+            if constexpr (FUSED) load_digits(ar[0], 0, 0);
             v4i acc[ND][NT];
 #pragma unroll
             for (int d = 0; d < ND; ++d)
@@ -439,7 +509,7 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
             for (int c = 0; c < 4; ++c) {
                 const int n = first + c;
                 if (n < a.batch) {
-                    const int ex = ND == 3 ? a.scalings[n].e3 : a.scalings[n].e4;
+                    const int ex = FUSED ? s_exponents[n % kGroupVectors] : (ND == 3 ? a.scalings[n].e3 : a.scalings[n].e4);
                     const double factor = ex == kNotFinite ? (double)NAN : ldexp(gscale, -ex);
                     float *out = a.out + ((size_t)split * a.batch + n) * a.cols;
 #pragma unroll
@@ -502,43 +572,47 @@ __global__ __launch_bounds__(256) void k_grad_join(const float *__restrict__ par
 
 // How a call is shared out; the workspace holds [scalings][digits][parts of the split sum]
 struct GradPlan {
-    int wm, blocks, ks, steps, splits, steps_per_split;
+    int wm, blocks, ks, steps, splits, steps_per_split, held;       // held: 0, or the digits are made by k_grad
     size_t digits_off, parts_off, bytes;
 };
 constexpr int kGradCus = 256;
 static GradPlan grad_plan(const Layout &L, int batch)
 {
     GradPlan p;
-    // (two waves along the vectors, 17 to 32 of them, were slower than two workgroups with one: 8192 x 8192, 32 vectors 32.8 us, 30.7)
-    p.wm = batch <= 32 ? 1 : (batch <= 64 ? 4 : 8);
-    p.blocks = L.cq * (p.wm == 8 ? 4 : (p.wm == 4 ? 2 : 1));
-    p.ks = p.wm == 8 ? 8 : (p.wm == 4 ? 4 : 2);
     p.steps = (L.rt_count + 3) / 4;
-    const int rows_of = (batch + 16 * p.wm - 1) / (16 * p.wm);
-    // Parts of the sum: rounds of workgroups over the chip (one per compute unit), each of so many us for its start and end and for a step; more
-    // than one part costs the way of the parts through memory and a launch.
-    const double step = p.wm == 8 ? 0.67 : (p.wm == 4 ? 0.75 : 1.5);
     double least_time = 1e30;
-    p.splits = 1;
-    for (int splits = (p.steps + 1023) / 1024, n = 0; n < 64; ++splits, ++n) {       // (int32 sums: 65536 rows)
-        const int each = ((p.steps + splits - 1) / splits + p.ks - 1) / p.ks * p.ks, parts = (p.steps + each - 1) / each;   // (whole buffers)
-        if (parts < splits && n) continue;
-        const double rounds = (double)(((long long)p.blocks * rows_of * parts + kGradCus - 1) / kGradCus);
-        const double time = rounds * (3.0 + step * each) + (parts > 1 ? 3.0 + (parts + 2) * 4e-6 * batch * L.cols / 4.0 : 0.0);
-        if (time < least_time) { least_time = time; p.splits = parts; p.steps_per_split = each; }
+    // (two waves along the vectors, 17 to 32 of them, were slower than two workgroups with one: 8192 x 8192, 32 vectors 32.8 us, 30.7)
+    for (int wm = batch <= 32 ? 1 : (batch <= 64 ? 4 : 8); wm; wm = wm > 1 ? 1 : 0) {
+        const int blocks = L.cq * (wm == 8 ? 4 : (wm == 4 ? 2 : 1)), ks = wm == 8 ? 8 : (wm == 4 ? 4 : 2);
+        const int rows_of = (batch + 16 * wm - 1) / (16 * wm), held = wm > 1 ? 0 : (batch <= 4 ? 4 : (batch <= 8 ? 8 : 16));
+        // Parts of the sum: rounds of workgroups over the chip (one per compute unit), each of so many us for its start and end and for a step; more
+        // than one part costs the way of the parts through memory and a launch, digits that do not fit a workgroup a launch or two.
+        const double step = wm == 8 ? 0.67 : (wm == 4 ? 0.75 : 1.5);
+        for (int splits = (p.steps + 1023) / 1024, n = 0; n < 64; ++splits, ++n) {       // (int32 sums: 65536 rows)
+            const int each = ((p.steps + splits - 1) / splits + ks - 1) / ks * ks, parts = (p.steps + each - 1) / each;   // (whole buffers)
+            if (parts < splits && n) continue;
+            const bool fits = held && each * held <= kFusedSteps * 4;
+            const double rounds = (double)(((long long)blocks * rows_of * parts + kGradCus - 1) / kGradCus);
+            const double time = (fits ? 0.0 : 4.0 + (batch > 16 ? 2.0 : 0.0)) + rounds * (3.0 + (fits ? 2.0 : 0.0) + step * each) +
+                                (parts > 1 ? 3.0 + (parts + 2) * 4e-6 * batch * L.cols / 4.0 : 0.0);
+            if (time < least_time) {
+                least_time = time;
+                p.wm = wm; p.blocks = blocks; p.ks = ks; p.splits = parts; p.steps_per_split = each; p.held = fits ? held : 0;
+            }
+        }
     }
     auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
     p.digits_off = up((size_t)batch * sizeof(Scaling));
-    p.parts_off = p.digits_off + (size_t)((batch + 15) / 16) * (size_t)p.steps * 4096;
+    p.parts_off = p.digits_off + (p.held ? 0 : (size_t)((batch + 15) / 16) * (size_t)p.steps * 4096);
     p.bytes = p.parts_off + (p.splits > 1 ? up((size_t)p.splits * batch * L.cols * 4) : 0);
     return p;
 }
 size_t grad_workspace_bytes(const Layout &L, int batch) { return grad_plan(L, batch).bytes; }
 
-#define PB_GRAD(WM) {{reinterpret_cast<const void *>(k_grad<1, false, WM>), reinterpret_cast<const void *>(k_grad<1, true, WM>)}, \
-                     {reinterpret_cast<const void *>(k_grad<2, false, WM>), reinterpret_cast<const void *>(k_grad<2, true, WM>)}}
-static const void *const kGradFn[3][2][2] = {PB_GRAD(1), PB_GRAD(4), PB_GRAD(8)};
-constexpr int kGradLds[3] = {GradShape<1>::LDS, GradShape<4>::LDS, GradShape<8>::LDS};
+#define PB_GRAD(WM, FUSED) {{reinterpret_cast<const void *>(k_grad<1, false, WM, FUSED>), reinterpret_cast<const void *>(k_grad<1, true, WM, FUSED>)}, \
+                            {reinterpret_cast<const void *>(k_grad<2, false, WM, FUSED>), reinterpret_cast<const void *>(k_grad<2, true, WM, FUSED>)}}
+static const void *const kGradFn[4][2][2] = {PB_GRAD(1, false), PB_GRAD(4, false), PB_GRAD(8, false), PB_GRAD(1, true)};
+constexpr int kGradLds[4] = {GradShape<1>::LDS, GradShape<4>::LDS, GradShape<8>::LDS, GradShape<1>::LDS + kFusedLds};
 
 int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, int bits_used, const float *dY, const GatedSource *gated,
                 int batch, float *dX, void *workspace, hipStream_t st)
@@ -550,21 +624,22 @@ int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, in
     // Whether the workgroups of the digits work the scalings out themselves: up to 128 KB of vectors each.  us with it / with a launch of its own:
     // 1024 x 1024, one vector 12.5 / 14.2; 2000 x 2000, 1000 vectors 35.1 / 37.9; 4096 x 4096, 64 vectors (256 KB) 28.9 / 28.1; 5460 x 1000, 40 (341 KB)
     // 21.3 / 19.7.
-    const bool own = !gated && (long long)(batch < 16 ? batch : 16) * L.rows <= 32768;
+    const bool own = !gated && !p.held && (long long)(batch < 16 ? batch : 16) * L.rows <= 32768;
     int err = 0;
     if (gated) {
         hipLaunchKernelGGL(k_gated_grad, dim3((unsigned)batch), dim3(1024), 0, st, gated->pre, gated->dH, L.rows / 2, gated->gate, gated->dpre,
                            scalings);
         dY = gated->dpre;
-    } else if (!own) {
+    } else if (!own && !p.held) {
         hipLaunchKernelGGL(k_grad_scalings, dim3((unsigned)batch), dim3(1024), 0, st, dY, L.rows, scalings);
     }
     err = (int)hipGetLastError();
     if (err) return err;
     const int waves = own ? 16 : 4, may_narrow = p.wm >= 4;
-    hipLaunchKernelGGL(own ? k_grad_digits<true> : k_grad_digits<false>,
-                       dim3((unsigned)((p.steps + waves - 1) / waves), (unsigned)((batch + 15) / 16)), dim3((unsigned)waves * 64), 0, st, dY,
-                       scalings, batch, L.rows, L.gate_h, p.steps, may_narrow, digits);
+    if (!p.held)
+        hipLaunchKernelGGL(own ? k_grad_digits<true> : k_grad_digits<false>,
+                           dim3((unsigned)((p.steps + waves - 1) / waves), (unsigned)((batch + 15) / 16)), dim3((unsigned)waves * 64), 0, st, dY,
+                           scalings, batch, L.rows, L.gate_h, p.steps, may_narrow, digits);
     err = (int)hipGetLastError();
     if (err) return err;
     GradArgs a;
@@ -575,13 +650,14 @@ int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, in
     a.rt_count = L.rt_count; a.cq = L.cq; a.m = bits_used; a.batch = batch; a.cols = L.cols;
     a.steps = p.steps; a.steps_per_split = p.steps_per_split;
     a.scales = scales; a.digits = digits; a.scalings = scalings; a.may_narrow = may_narrow;
+    a.dY = dY; a.rows = L.rows; a.gate_h = L.gate_h; a.held = p.held;
     a.blocks = p.blocks; a.rows_of = (batch + 16 * p.wm - 1) / (16 * p.wm);
     a.workgroups = a.blocks * a.rows_of * p.splits;
     float *const parts = reinterpret_cast<float *>(ws + p.parts_off);
     a.out = p.splits > 1 ? parts : dX;
-    const int shape = p.wm == 8 ? 2 : p.wm / 4, wide = bits_used > 4, il = is_pairs(L.layout);
+    const int shape = p.held ? 3 : (p.wm == 8 ? 2 : p.wm / 4), wide = bits_used > 4, il = is_pairs(L.layout);
     const void *fn = kGradFn[shape][wide][il];
-    static bool declared[3][2][2];      // (more than the default 64 KB of LDS)
+    static bool declared[4][2][2];      // (more than the default 64 KB of LDS)
     hipError_t e = hipSuccess;
     if (!__atomic_load_n(&declared[shape][wide][il], __ATOMIC_RELAXED)) {
         e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kGradLds[shape]);
