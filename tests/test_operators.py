@@ -195,6 +195,20 @@ def test_gradient_through_the_packed_matrix(pb, rows, cols, bits, m, batch, layo
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols,batches", [(520, 32768, (2, 7)), (40000, 40, (3, 7, 12, 20))])
+def test_gradient_of_few_vectors_and_many_rows_or_columns(pb, rows, cols, batches):
+    """Parts of the sum of more than eight steps of 64 rows; digits that do not fit a workgroup."""
+    layer = Layer(pb, rows, cols, 1)
+    W = layer.matrix(1)
+    for batch in batches:
+        dY = (np.random.default_rng(13).standard_normal((batch, rows)) * 10.0 ** np.arange(batch)[:, None]).astype(np.float32)
+        dX = layer.lin.grad(torch.from_numpy(dY).cuda())
+        d64 = dY.astype(np.float64)
+        # at most 64 parts
+        close(dX, d64 @ W, grad_tolerance(d64, W, 64), "dX")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("batch", [3, 20, 70])
 @pytest.mark.parametrize("bits,m", [(3, 3), (6, 6)])
 @pytest.mark.parametrize("layout", ["bits", "pairs"])
@@ -365,6 +379,9 @@ ADAPTED = [  # rows, cols, bits, used, batch, layout, count, rank, type, index
     (64, 300, 8, 8, 17, "bits", 2, 200, "f16", "mixed"), (1030, 64, 8, 8, 3, "bits", 300, 5, "f32", "mixed"), (64, 1030, 8, 8, 2, "bits", 4096, 3, "bf16", "mixed"),
     (40, 60, 2, 2, 4096, "bits", 7, 4, "f32", "mixed"), (40, 60, 2, 2, 1000, "bits", 1000, 4, "bf16", "mixed"), (60, 40, 8, 8, 50, "gates", 3, 12, "f16", "mixed"),
     (200, 90, 8, 8, 48, "bits", 5, 16, "bf16", "outside"), (33, 70, 3, 3, 4, "rows", 2, 4, "f32", "mixed"), (200, 2100, 8, 8, 100, "bits", 3, 20, "bf16", "mixed"),
+    # sums in eight and in sixteen parts; several turns over the ranks; one adapter with all vectors beside many with none
+    (200, 5000, 2, 2, 70, "bits", 2, 33, "bf16", "mixed"), (5000, 64, 2, 2, 20, "bits", 3, 50, "f32", "mixed"), (130, 300, 4, 4, 30, "bits", 2, 90, "f16", "mixed"),
+    (70, 700, 8, 8, 200, "bits", 100, 24, "f16", "same"), (64, 300, 8, 8, 50, "bits", 40, 70, "bf16", "same"), (515, 320, 4, 4, 200, "bits", 1, 36, "bf16", "none"),
 ]
 
 
