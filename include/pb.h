@@ -262,7 +262,7 @@ int pb_lstm_cell(const void *packed, const float *scales, const pb_desc *d, int 
  *   pre   [batch][2F] or NULL: the pre-activations [g ; u], written (what the backward pass needs)
  *   workspace: pb_workspace_bytes(d, batch) bytes, overwritten
  * No output may overlap another one or an input.  PB_EINVAL if rows is odd.  With PB_LAYOUT_TILE16_GATES_V1 (F even) the product and
- * the gate are one launch where there are few vectors: its row tiles hold rows r, F/2 + r, F + r, 3F/2 + r next to each other, the gates and the values of two units. */
+ * the gate are one launch: its row tiles hold rows r, F/2 + r, F + r, 3F/2 + r next to each other, the gates and the values of two units. */
 typedef enum pb_gate { PB_GATE_SIGMOID = 0, PB_GATE_SILU = 1, PB_GATE_GELU = 2, PB_GATE_RELU = 3 } pb_gate;
 int pb_gated_linear(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *X, int batch,
                     const float *bias, int gate, float *H, float *pre, void *workspace, void *stream);
@@ -270,10 +270,11 @@ int pb_gated_linear(const void *packed, const float *scales, const pb_desc *d, i
 /* Gradient of pb_matmul with respect to its activations, the packed matrix being frozen:
  *   dX[n][c] = sum_r dY[n][r] w[r][c],   w = sum_{i < bits_used} scales[i] * bit_i,
  * with the same bits_used as in the forward call; the conversion to fixed point counts as the identity (frac_bits and act_bits do
- * not matter).  dY enters as integers of 31 bits of its vector's largest magnitude, the sums of products are exact and
- * rounded to fp32 (more than 1024 steps of 64 rows, more than eight bitlayers, few vectors: a few such sums are added in fp32, in the same
- * order every time).  A vector with a value that is not finite gets NaN everywhere.
- *   dY  [batch][rows] fp32, read only;  dX  [batch][cols] fp32, written
+ * not matter).  dY enters as integers: off by at most 2^-30 of its vector's largest magnitude, or 2^-23 of it in groups of sixteen vectors of
+ * batches above 32 where no value is above 12 sqrt(max(1, rows / 4096)) times the root of its vector's mean square.  The sums of products are exact
+ * and rounded to fp32; where the sum over the rows is shared out, and for more than eight bitlayers, a few such sums are added in fp32, in the same
+ * order every time.  A vector with a value that is not finite gets NaN everywhere.
+ *   dY  [batch][rows] fp32, read only;  dX  [batch][cols] fp32, written; they do not overlap
  *   workspace: pb_grad_workspace_bytes(d, batch) bytes, overwritten (0 for what the call does not take)
  * Tiled layouts only (PB_EINVAL for PB_LAYOUT_ROWMAJOR_V1). */
 size_t pb_grad_workspace_bytes(const pb_desc *d, int batch);
@@ -295,7 +296,7 @@ typedef enum pb_type { PB_TYPE_F32 = 0, PB_TYPE_BF16 = 1, PB_TYPE_F16 = 2 } pb_t
 #define PB_MAX_ADAPTERS 4096
 #define PB_MAX_RANK 256
 typedef struct pb_adapters {
-    int32_t count, rank, type, reserved;   /* reserved: 0 */
+    int32_t count, rank, type, reserved;   /* 1 .. PB_MAX_ADAPTERS, 1 .. PB_MAX_RANK, a pb_type, 0 */
     const void *A, *B;
     const float *scale;
 } pb_adapters;
@@ -304,7 +305,7 @@ typedef struct pb_adapters {
  *   Y[n] = (the product of pb_matmul for x_n) + bias + scale[k] B_k (A_k x_n),   k = index[n].
  * The adapters' products take x as it is (not its fixed-point value) and run in fp32, whatever the adapters' type.
  *   index  [batch] int32, in any order; a vector whose index is outside [0, count) has no adapter.  NULL: adapter 0 for all
- *   bias   [rows] or NULL;  Y  [batch][rows] fp32, written
+ *   bias   [rows] or NULL;  Y  [batch][rows] fp32, written, not overlapping an input
  *   workspace: pb_adapters_workspace_bytes(d, adapters, batch) bytes, overwritten (0 for a shape that is refused) */
 size_t pb_adapters_workspace_bytes(const pb_desc *d, const pb_adapters *adapters, int batch);
 int pb_matmul_adapters(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *X, int batch,

@@ -430,7 +430,7 @@ int pb_gated_linear_grad(const void *packed, const float *scales, const pb_desc 
 
 static int check_adapters(const pb_adapters *ad)
 {
-    if (!ad || !ad->A || !ad->B || ad->count < 1 || ad->rank < 1) return PB_EINVAL;
+    if (!ad || !ad->A || !ad->B || ad->count < 1 || ad->rank < 1 || ad->reserved != 0) return PB_EINVAL;
     if (ad->type < PB_TYPE_F32 || ad->type > PB_TYPE_F16) return PB_EINVAL;
     if (ad->count > PB_MAX_ADAPTERS || ad->rank > PB_MAX_RANK) return PB_ESIZE;
     return aligned16(ad->A) && aligned16(ad->B) && aligned16(ad->scale) ? PB_OK : PB_EALIGN;

@@ -78,6 +78,14 @@ def test_arguments_rejected_before_launch(pb):
     assert L.pb_matmul_adapters(fake, fake, ref(d), 4, fake, 1, None, fake, null, fake, fake, null) == pb.PB_EINVAL
 
 
+def test_a_reserved_field_that_is_set_is_refused(pb):
+    d, fake, null = pb.pb_desc_init(64, 96, 4), ctypes.c_void_p(0x1000), ctypes.c_void_p(0)
+    a = pb.pb_adapters(2, 3, pb.PB_TYPE_F32, 1, 0x1000, 0x1000, None)
+    L, ref = pb.lib(), ctypes.byref
+    assert L.pb_matmul_adapters(fake, fake, ref(d), 4, fake, 1, ref(a), null, null, fake, fake, null) == pb.PB_EINVAL
+    assert L.pb_matmul_adapters_grad(fake, fake, ref(d), 4, fake, fake, 1, ref(a), null, fake, fake, fake, fake, null) == pb.PB_EINVAL
+
+
 def test_workspace_sizes(pb):
     d, rows = pb.pb_desc_init(4096, 1000, 8), pb.pb_desc_init_layout(64, 96, 4, pb.PB_LAYOUT_ROWMAJOR_V1)
     assert pb.pb_grad_workspace_bytes(rows, 1) == 0 and pb.pb_grad_workspace_bytes(d, 0) == 0
