@@ -739,9 +739,15 @@ int launch_adapter_grads(const AdapterPlan &p, const pb_adapters &ad, const Layo
     B = A;
     A.scale = nullptr; A.parts = reinterpret_cast<const float *>(ws + p.t_off); A.V = X; A.out = dA; A.length = L.cols;
     B.scale = ad.scale; B.parts = reinterpret_cast<const float *>(ws + p.u_off); B.V = dY; B.out = dB; B.length = L.rows;
-    // Adapters of many vectors are split over the waves along those (by the mean: where the vectors' adapters are is known on the device only)
-    const bool split = batch > kMany * ad.count;
-    const int rt = split ? (p.ranks == 1 ? 1 : 2) : rank_tiles(p.ranks), columns = split ? 64 : 64 * outer_waves(false);
+    // Whether the waves of a workgroup share an adapter's vectors, by an estimate in us from the mean of them (which adapters the vectors have is known on
+    // the device only): rounds of workgroups, one or two on a compute unit, against the turns over the vectors of a wave alone.  us, shared / alone:
+    // 6453 + 2048 rows and columns, 3 adapters of rank 50, 498 vectors 29 / 37; 8845 + 1106, 1 of 19, 1568 29 / 222; 4096 + 4096, 4 of 16, 2048 15 / 58;
+    // but 8438 + 4091, 6 of 49, 471 60 / 30; 4096 + 4096, 16 of 64, 1024 91 / 26; 8 of 16, 512 16 / 12.
+    const int shared_rt = p.ranks == 1 ? 1 : 2, alone_rt = rank_tiles(p.ranks);
+    const long long groups = (long long)((dA ? (L.cols + 63) / 64 : 0) + (dB ? (L.rows + 63) / 64 : 0)) * ad.count * ((p.ranks + shared_rt - 1) / shared_rt);
+    const double mean = (double)batch / ad.count, rounds = (double)((groups + 512 / shared_rt - 1) / (512 / shared_rt));
+    const bool split = batch > kMany && rounds * (5.5 + mean / 64) < 4.0 + mean / 8 * (0.75 + 0.25 * alone_rt);
+    const int rt = split ? shared_rt : alone_rt, columns = split ? 64 : 64 * outer_waves(false);
     static const void *const fns[2][4] = {{reinterpret_cast<const void *>(k_adapter_outer<false, 1>), reinterpret_cast<const void *>(k_adapter_outer<false, 2>),
                                            reinterpret_cast<const void *>(k_adapter_outer<false, 3>), reinterpret_cast<const void *>(k_adapter_outer<false, 4>)},
                                           {reinterpret_cast<const void *>(k_adapter_outer<true, 1>), reinterpret_cast<const void *>(k_adapter_outer<true, 2>)}};
