@@ -6,6 +6,8 @@
 // one into codes, step by step between the products.  Per chunk and wave: 8 KB of words and 24 KB of digits (three of four, see pb_imma.h) from
 // memory, 64 KB of codes from LDS, 192 matrix instructions.
 // Bound: the matrix instructions (16 cycles each); LDS and the vector-memory pipeline are busy for about three quarters of that.
+// us: 8192 x 4096, 8 bitlayers, 2048 vectors 196 (2.10 POP/s in three digits); a gated block of 21844 x 4096, 1024 vectors 286 (1.92 POP/s; its 1368
+// workgroups are 5.3 rounds over the chip).
 #include <type_traits>
 
 #include "pb_imma.h"

@@ -1,4 +1,5 @@
-// The gate of a gated block on pre-activations that the product left in memory, for the layouts whose product kernels have no such epilogue.
+// The gate of a gated block on pre-activations that the product left in memory, for the layouts and shapes whose product kernels have no such epilogue.
+// Bound: the launch for what comes here (18090 x 76 values, 5.5 MB: 4.9 us), else memory.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

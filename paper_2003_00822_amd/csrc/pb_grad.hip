@@ -10,9 +10,17 @@
 // 12 * 2^-22 / sqrt(12) = 8e-7 sqrt(max(1, R / 4096)) of the results' root mean square at most, typically a quarter of it.  (A product in fp32 is
 // off by 1.75e-8 sqrt(R), measured from 1500 to 21844 rows: 1.1e-6 at 4096.)
 //
+// Few vectors (and small matrices): k_grad makes the digits itself, from the rows of its part of the sum; each part has a scale of its own, and the parts
+// are added in fp32 anyway.  Else k_grad_digits leaves them in memory, for all of the columns' workgroups.
+//
 // The sum runs over the rows of W, and a packed word holds 32 columns of one row: the codes have to be turned, 16 rows of a column
 // into the 16 bytes of a lane.  They go through LDS anyway, because every wave needs them, and DS_READ_B64_TR_B8 turns them on the
 // way out: its 16 lanes read eight rows of sixteen bytes, and lane i receives byte i of each.
+//
+// Bound: the packed words for few vectors, the matrix instructions for batches.  us (rocprofv3): 8192 x 8192, 8 bitlayers, 4 vectors: k_grad 17.0 (3.9 TB/s
+// of words) and k_grad_join 3.9; 6 bitlayers, 768 vectors: k_grad 138 (2.25 POP/s in three digits; a library product of 8-bit integers of that
+// size reaches 1.83), scalings 7.5, digits 8.3, join 14.4; 21844 x 4096, 8 bitlayers, 1024 vectors: k_grad 261 (2.1 POP/s), k_gated_grad 40 (224 MB,
+// 5.6 TB/s), digits 31 (157 MB, 5.0 TB/s).
 #include <type_traits>
 
 #include "pb_imma.h"
@@ -581,7 +589,10 @@ static GradPlan grad_plan(const Layout &L, int batch)
     GradPlan p;
     p.steps = (L.rt_count + 3) / 4;
     double least_time = 1e30;
-    // (two waves along the vectors, 17 to 32 of them, were slower than two workgroups with one: 8192 x 8192, 32 vectors 32.8 us, 30.7)
+    // The shape: one wave along the vectors for up to 32, four for up to 64, eight for more, or one all the same where that is estimated to be faster
+    // (the digits then need no launch).  us, digits in launches of their own / in k_grad: 670 x 2642, 71 vectors 20.0 / 13.8; 1024 x 1024, 128 vectors
+    // 18.4 / 13.7; 2048 x 2048, 48 vectors 20.0 / 14.6; 801 x 1549, 282 vectors 21.0 / 16.1; 8192 x 8192, 4 vectors 27.3 / 20.3; 4096 x 4096, 16 vectors
+    // 22.0 / 17.1.  (Two waves along 17 to 32 vectors were slower than two workgroups with one: 8192 x 8192, 32 vectors 32.8, 30.7.)
     for (int wm = batch <= 32 ? 1 : (batch <= 64 ? 4 : 8); wm; wm = wm > 1 ? 1 : 0) {
         const int blocks = L.cq * (wm == 8 ? 4 : (wm == 4 ? 2 : 1)), ks = wm == 8 ? 8 : (wm == 4 ? 4 : 2);
         const int rows_of = (batch + 16 * wm - 1) / (16 * wm), held = wm > 1 ? 0 : (batch <= 4 ? 4 : (batch <= 8 ? 8 : 16));
@@ -622,8 +633,8 @@ int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, in
     Scaling *const scalings = reinterpret_cast<Scaling *>(ws);
     uint8_t *const digits = reinterpret_cast<uint8_t *>(ws + p.digits_off);
     // Whether the workgroups of the digits work the scalings out themselves: up to 128 KB of vectors each.  us with it / with a launch of its own:
-    // 1024 x 1024, one vector 12.5 / 14.2; 2000 x 2000, 1000 vectors 35.1 / 37.9; 4096 x 4096, 64 vectors (256 KB) 28.9 / 28.1; 5460 x 1000, 40 (341 KB)
-    // 21.3 / 19.7.
+    // 2000 x 2000, 1000 vectors 35.6 / 38.2; 4096 columns, 1000 rows, 1000 vectors 27.2 / 29.7; 2048 x 2048, 256 vectors 24.4 / 24.2; but 1800 columns, 4100
+    // rows, 104 vectors (262 KB) 24.4 / 23.2; 4096 x 4096, 64 vectors (262 KB) 29.2 / 28.4.
     const bool own = !gated && !p.held && (long long)(batch < 16 ? batch : 16) * L.rows <= 32768;
     int err = 0;
     if (gated) {

@@ -258,7 +258,7 @@ struct I8Args {
 };
 
 // What a kernel does with the sums: store Y (bias and ReLU first), update the LSTM cell, store the sums themselves, a gated block's
-// act(g) u (k_gated_stream)
+// act(g) u (k_gated_stream, k_gated_tile, k_batch)
 enum { kStore = 0, kCell = 1, kSums = 2, kGated = 3 };
 
 // Whether one of the values of so many quads of vectors needs four digits (the lanes see one chunk each: there are at most 64)

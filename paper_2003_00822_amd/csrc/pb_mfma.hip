@@ -185,6 +185,7 @@ __device__ __forceinline__ v4f mfma_fp4(const v8i a, const v8i b, const v4f c)
 // the registers a wave may use; RU: units (row tile, bitlayer) whose blocks a wave has in flight.  The host picks
 // RU <= the units a wave has, so that a short stream pays for no empty ring slots; 4 KB in flight per wave
 // measured best (more requests in flight than that slow the short streams down and do not speed up the long ones).
+// GATED: act(g) u of a gated block behind the product, in the same launch (5460 x 1024 on the gate layout, 4 bitlayers: 4.3 us)
 template <int NQ, int MAXS, int RU, bool GATED = false>
 __global__ __launch_bounds__(MAXS * 64) void k_mfma(const uint32_t *packed, const float *X0, uint32_t packed_bytes,
                                                     uint32_t flags, int cols0, uint32_t layer_step,
