@@ -721,6 +721,12 @@ static int launch_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &
     });
 }
 
+AdapterRows adapter_rows(const AdapterPlan &p, const pb_adapters &ad, const int32_t *index, void *workspace)
+{
+    return {ad.B, ad.scale, reinterpret_cast<const float *>(static_cast<char *>(workspace) + p.u_off), index, ad.rank, ad.count, ad.type,
+            down_parts(p.slices)};
+}
+
 int launch_adapter_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, int batch, float *Y, void *workspace,
                       hipStream_t st)
 {

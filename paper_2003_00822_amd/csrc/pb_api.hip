@@ -474,8 +474,12 @@ int pb_matmul_adapters(const void *packed, const float *scales, const pb_desc *d
     pb::Epilogue ep;
     ep.bias = bias;
     ep.pre = reinterpret_cast<float *>(static_cast<char *>(workspace) + pb::ws_gates_off(L, batch));
+    // (one vector: B_k u behind the product, a launch less)
+    const pb::AdapterRows rows = pb::adapter_rows(p, *adapters, index, ws);
+    const bool behind = batch == 1 && pb::is_tile16(L.layout) && !pb::takes_digits(L, batch) && adapters->rank <= pb::kAdapterRowsRank;
+    if (behind) ep.adapter = &rows;
     rc = matmul_common(packed, scales, d, bits_used, X, d->cols, nullptr, 0, batch, Y, nullptr, workspace, stream, ep, false, true);
-    if (rc != PB_OK) return rc;
+    if (rc != PB_OK || behind) return rc;
     return hip_status(pb::launch_adapter_up(p, *adapters, L, index, batch, Y, ws, st));
 }
 

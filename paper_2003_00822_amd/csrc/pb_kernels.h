@@ -29,6 +29,14 @@ int launch_matvec(const uint32_t *packed, const float *scales, const Layout &L, 
 // What follows the product in the same launch: bias and ReLU before the store of Y, or (PB_LAYOUT_TILE16_GATES_V1
 // only) the LSTM cell update, which writes h_out / c_out [batch][H] instead of Y, or a gated block's act(g) u, which writes
 // h_out [batch][rows / 2] and, where wanted, the pre-activations to Y.
+// What a single vector's adapter adds to it in k_mfma: scale_k B_k u, u being there in parts (pb_adapters.hip)
+struct AdapterRows {
+    const void *B;
+    const float *scale, *parts;
+    const int32_t *index;
+    int rank, count, type, nparts;
+};
+constexpr int kAdapterRowsRank = 16;     // (32 cost scratch memory in two of the kernels)
 struct Epilogue {
     const float *bias = nullptr;   // [rows] or null
     int relu = 0;
@@ -36,6 +44,7 @@ struct Epilogue {
     float *h_out = nullptr, *c_out = nullptr;
     int gate = -1;                 // 0 or more: fused gated block (a pb_gate)
     float *pre = nullptr;          // non-null: room for [batch][rows], and the kernel for large batches of pb_batch.hip may be taken
+    const AdapterRows *adapter = nullptr;   // (one vector, tiled layouts but the pairs')
     bool fused() const { return c_prev || gate >= 0; }
 };
 int launch_mfma(const uint32_t *packed, const float *scales, const Layout &L, int bits_used, int frac_bits,
@@ -96,7 +105,8 @@ int launch_adapter_order(const AdapterPlan &p, const pb_adapters &ad, const int3
 // u = A_k x (and t = scale_k B_k^T dY, if dY is given) of the ordered vectors, in parts
 int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, const float *X, const float *dY, int batch,
                         void *workspace, hipStream_t st);
-// Y += scale_k B_k u
+// Y += scale_k B_k u; what launch_mfma needs to do it for one vector
+AdapterRows adapter_rows(const AdapterPlan &p, const pb_adapters &ad, const int32_t *index, void *workspace);
 int launch_adapter_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, int batch, float *Y, void *workspace,
                       hipStream_t st);
 // dX += A_k^T t (if dX is given), dA_k = sum t x^T, dB_k = scale_k sum dy u^T (where given)

@@ -82,8 +82,10 @@ struct MfmaArgs {
     float fscale;               // 2^frac_bits
     int imin, imax;             // range of the act_bits-bit fixed-point values
     double out_scale;           // 2^-frac_bits
-    int gate;                   // (GATED) act(g) u of a gated block goes to h_out, the pre-activations to Y if that is non-null
+    int gate;                   // (kGatedBlock) act(g) u of a gated block goes to h_out, the pre-activations to Y if that is non-null
+    AdapterRows adapter;        // (kAdapted)
 };
+enum { kPlain = 0, kGatedBlock = 1, kAdapted = 2 };
 
 // z + (z of the lane D lanes away, D = 16 or 32), in both lanes
 template <int D>
@@ -181,12 +183,60 @@ __device__ __forceinline__ v4f mfma_fp4(const v8i a, const v8i b, const v4f c)
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, 0, 127, 0, 127);
 }
 
+// The adapter's rows (kAdapted), up to rank 16.  Lane 16 lg + j has matrix row j of the row tile and the ranks 4 lg .. 4 lg + 3 of it, and brings the parts
+// 4 lg .. 4 lg + 3 of u for rank j.  What lies beyond is another's and not used.
+template <int MORE>
+struct AdapterOfRow {
+    __device__ __forceinline__ void request(const MfmaArgs &, int, int) {}
+    __device__ __forceinline__ float value(const MfmaArgs &, int) const { return 0.0f; }
+};
+template <>
+struct AdapterOfRow<kAdapted> {
+    uint32_t b[4];
+    float4 u;
+    __device__ __forceinline__ void request(const MfmaArgs &a, int lane, int row)
+    {
+        const AdapterRows &ad = a.adapter;
+        const int lg = lane >> 4, given = ad.index ? ad.index[0] : 0, k = given >= 0 && given < ad.count ? given : 0;
+        const size_t at = ((size_t)k * a.R + row) * ad.rank;
+        u = *reinterpret_cast<const float4 *>(ad.parts + (lane & 15) * ad.nparts + (4 * lg < ad.nparts ? 4 * lg : 0));
+        if (ad.type == PB_TYPE_F32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) b[e] = static_cast<const uint32_t *>(ad.B)[at + min(4 * lg + e, ad.rank - 1)];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) b[e] = static_cast<const uint16_t *>(ad.B)[at + min(4 * lg + e, ad.rank - 1)];
+        }
+    }
+    // (in all lanes of the row)
+    __device__ __forceinline__ float value(const MfmaArgs &a, int lane) const
+    {
+        const AdapterRows &ad = a.adapter;
+        const int lg = lane >> 4, given = ad.index ? ad.index[0] : 0;
+        float v = 4 * lg < ad.nparts ? (u.x + u.y) + (u.z + u.w) : 0.0f, sum = 0.0f;
+        v += __shfl_xor(v, 16);
+        v += __shfl_xor(v, 32);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float w = ad.type == PB_TYPE_F32 ? __uint_as_float(b[e])
+                                                   : (ad.type == PB_TYPE_BF16 ? __uint_as_float(b[e] << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)b[e]));
+            const float x = __shfl(v, 4 * lg + e);
+            if (4 * lg + e < ad.rank) sum = fmaf(w, x, sum);
+        }
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (given < 0 || given >= ad.count) return 0.0f;
+        return ad.scale ? sum * ad.scale[given] : sum;
+    }
+};
+
 // NQ: chunks of 512 columns per wave; MAXS: most waves (column slices) per workgroup, which bounds
 // the registers a wave may use; RU: units (row tile, bitlayer) whose blocks a wave has in flight.  The host picks
 // RU <= the units a wave has, so that a short stream pays for no empty ring slots; 4 KB in flight per wave
 // measured best (more requests in flight than that slow the short streams down and do not speed up the long ones).
-// GATED: act(g) u of a gated block behind the product, in the same launch (5460 x 1024 on the gate layout, 4 bitlayers: 4.3 us)
-template <int NQ, int MAXS, int RU, bool GATED = false>
+// MORE: kGatedBlock, act(g) u of a gated block behind the product, in the same launch (5460 x 1024 on the gate layout, 4 bitlayers: 4.3 us);
+// kAdapted, the rows of an adapter's B times its u (1024 x 1024, 8 bitlayers, rank 8 in bf16: 5.3 us; without 4.5 and then k_adapter_up 3.6).
+template <int NQ, int MAXS, int RU, int MORE = kPlain>
 __global__ __launch_bounds__(MAXS * 64) void k_mfma(const uint32_t *packed, const float *X0, uint32_t packed_bytes,
                                                     uint32_t flags, int cols0, uint32_t layer_step,
                                                     uint32_t round_step, int rounds_per_wg, int rt_count, int cq,
@@ -444,6 +494,8 @@ __global__ __launch_bounds__(MAXS * 64) void k_mfma(const uint32_t *packed, cons
                         const bool cell = row_ok && (lane & 3) == 0;
                         const float c_old =
                             __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rc, cell ? row * 4 : kNoOutput, 0, 0));
+                        AdapterOfRow<MORE> adapter;
+                        if constexpr (MORE == kAdapted) adapter.request(a, lane, row_ok ? row : 0);
                         double z = 0.0;
                         // the quarters of the vector: digits 0, 2, 4, 6 in units of 1, digits 8 .. 14 in units
                         // of 4^8, digits 1 .. 7 in units of 4, digits 9 .. 15 in units of 4^9; each below 2^31 in
@@ -487,6 +539,7 @@ __global__ __launch_bounds__(MAXS * 64) void k_mfma(const uint32_t *packed, cons
                         if (!a.A) {
                             float y = (float)(z * a.out_scale);
                             if (a.bias && row_ok) y += bias_row;
+                            if constexpr (MORE == kAdapted) y += adapter.value(a, lane);
                             if (a.c_prev) {
                                 // LSTM cell: the four lanes of a quad hold the gates i, f, g, o of one unit (row =
                                 // unit for gate i)
@@ -496,7 +549,7 @@ __global__ __launch_bounds__(MAXS * 64) void k_mfma(const uint32_t *packed, cons
                                     a.c_out[row] = cn;
                                     a.h_out[row] = hn;
                                 }
-                            } else if (GATED) {
+                            } else if (MORE == kGatedBlock) {
                                 // the first two lanes of a quad hold the gates of two units, the others their values
                                 const float hn = gated_quad(a.gate, y);
                                 if (row_ok && lg == 0) {
@@ -523,9 +576,11 @@ struct Variant {
     int nq, maxs, ru;
     const void *fn;
     const void *gated;     // with act(g) u of a gated block behind the product
+    const void *adapted;   // with an adapter's rows
 };
 #define PB_VARIANT(NQ, MAXS, RU) \
-    {NQ, MAXS, RU, reinterpret_cast<const void *>(k_mfma<NQ, MAXS, RU>), reinterpret_cast<const void *>(k_mfma<NQ, MAXS, RU, true>)}
+    {NQ, MAXS, RU, reinterpret_cast<const void *>(k_mfma<NQ, MAXS, RU>), reinterpret_cast<const void *>(k_mfma<NQ, MAXS, RU, kGatedBlock>), \
+     reinterpret_cast<const void *>(k_mfma<NQ, MAXS, RU, kAdapted>)}
 static const Variant kVariants[] = {
     PB_VARIANT(1, 16, 1), PB_VARIANT(1, 16, 2), PB_VARIANT(1, 16, 4),
     PB_VARIANT(2, 16, 1), PB_VARIANT(2, 16, 2), PB_VARIANT(2, 16, 3),
@@ -602,7 +657,7 @@ static int resident_workgroups(int variant, int S)
         for (int i = 0; i < kNumVariants; ++i) {
             const Variant &o = kVariants[i];
             if (o.nq != kVariants[variant].nq || o.maxs != kVariants[variant].maxs) continue;
-            for (const void *fn : {o.fn, o.gated})
+            for (const void *fn : {o.fn, o.gated, o.adapted})
                 if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)stage_bytes(S)) != hipSuccess) return 0;
         }
     }
@@ -651,7 +706,8 @@ int launch_mfma(const uint32_t *packed, const float *scales, const Layout &L, in
     const Variant &run = kVariants[pick_ring(vi, h.rounds_per_wg * bits_used)];
     void *args[] = {&h.packed, &h.X0, &h.packed_bytes, &h.flags, &h.cols0, &h.layer_step, &h.round_step,
                     &h.rounds_per_wg, &h.rt_count, &h.cq, &h.m, &a};
-    const hipError_t e = hipLaunchKernel(ep.gate >= 0 ? run.gated : run.fn, dim3((unsigned)wgs), dim3((unsigned)S * 64), args,
+    a.adapter = ep.adapter ? *ep.adapter : AdapterRows{};
+    const hipError_t e = hipLaunchKernel(ep.gate >= 0 ? run.gated : (ep.adapter ? run.adapted : run.fn), dim3((unsigned)wgs), dim3((unsigned)S * 64), args,
                                          planes ? 0 : stage_bytes(S), st);
     return (int)(e != hipSuccess ? e : hipGetLastError());
 }

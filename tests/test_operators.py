@@ -390,6 +390,9 @@ ADAPTED = [  # rows, cols, bits, used, batch, layout, count, rank, type, index
     # sums in eight and in sixteen parts; several turns over the ranks; one adapter with all vectors beside many with none
     (200, 5000, 2, 2, 70, "bits", 2, 33, "bf16", "mixed"), (5000, 64, 2, 2, 20, "bits", 3, 50, "f32", "mixed"), (130, 300, 4, 4, 30, "bits", 2, 90, "f16", "mixed"),
     (70, 700, 8, 8, 200, "bits", 100, 24, "f16", "same"), (64, 300, 8, 8, 50, "bits", 40, 70, "bf16", "same"), (515, 320, 4, 4, 200, "bits", 1, 36, "bf16", "none"),
+    # one vector
+    (333, 700, 8, 8, 1, "bits", 5, 16, "f16", "same"), (60, 5000, 4, 4, 1, "bits", 3, 13, "f32", "none"), (600, 2100, 8, 3, 1, "gates", 2, 15, "bf16", "same"),
+    (333, 700, 8, 8, 1, "bits", 5, 17, "bf16", "same"), (40, 9000, 2, 2, 1, "bits", 2, 4, "bf16", "outside"), (70, 300, 8, 8, 1, "pairs", 2, 16, "f16", "same"),
 ]
 
 
