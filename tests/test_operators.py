@@ -685,3 +685,156 @@ def test_native_and_python_operators_agree(pb):
     b.adapters.A = A[:, :, :10].contiguous()
     with pytest.raises(ValueError, match="another type or shape"):
         b.down.adapted(H, b.adapters, b.index)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 70])
+def test_nothing_else_is_written_for_one_vector_and_for_many(pb, n):
+    c = AdapterCase(pb, 90, 150, 8, 8, n, "bits", 3, 6, "f16", "same")
+    lin, d, desc = c.layer.lin, c.layer.lin.desc, c.adapters.desc()
+    X, dY, index = c.X.cuda(), c.dY.cuda(), c.index.cuda()
+    Y, dX, dA, dB = (torch.full(s, 7.0, device="cuda") for s in ((n + 2, 90), (n + 2, 150), (4, 6, 150), (4, 90, 6)))
+    size, grad_size = pb.pb_adapters_workspace_bytes(d, desc, n), pb.pb_grad_workspace_bytes(d, n)
+    ws, grad_ws = (torch.full((s + 256,), 0xA5, dtype=torch.uint8, device="cuda") for s in (size, grad_size))
+    pb.pb_matmul_adapters(lin.packed, lin.scales, d, 8, X, n, desc, index, None, Y, ws)
+    pb.pb_matmul_adapters_grad(lin.packed, lin.scales, d, 8, X, dY, n, desc, index, dX, dA, dB, ws)
+    torch.cuda.synchronize()
+    assert (ws[size:] == 0xA5).all()
+    for out, rows in ((Y, n), (dX, n), (dA, 3), (dB, 3)):
+        assert (out[rows:] == 7.0).all() and not (out[:rows] == 7.0).all()
+    dX.fill_(7.0)
+    pb.pb_matmul_grad(lin.packed, lin.scales, d, 8, dY, n, dX, grad_ws)
+    torch.cuda.synchronize()
+    assert (grad_ws[grad_size:] == 0xA5).all() and (dX[n:] == 7.0).all() and not (dX[:n] == 7.0).all()
+
+
+@pytest.mark.gpu
+def test_adapters_beyond_32_bits(pb):
+    """2.5e9 values of A, the last adapter used."""
+    count, rank, rows, cols = 300, 256, 40, 32768
+    layer = Layer(pb, rows, cols, 1)
+    g = torch.Generator().manual_seed(3)
+    a, b = (torch.randn(s, generator=g) * 0.1 for s in ((rank, cols), (rows, rank)))
+    A, B = (torch.zeros(s, dtype=torch.bfloat16, device="cuda") for s in ((count, rank, cols), (count, rows, rank)))
+    A[-1], B[-1] = a.cuda(), b.cuda()
+    X, dY = torch.randn((3, cols), generator=g), torch.randn((3, rows), generator=g)
+    index = torch.tensor([count - 1, -1, count - 1], dtype=torch.int32, device="cuda")
+    adapters = pb.Adapters(A, B)
+    Y = layer.lin.adapted(X.cuda(), adapters, index)
+    dX, dA, dB = layer.lin.adapted_grad(X.cuda(), dY.cuda(), adapters, index)
+    x, dy, a, b, W = X.double().numpy(), dY.double().numpy(), A[-1].double().cpu().numpy(), B[-1].double().cpu().numpy(), layer.matrix(1)
+    on = np.array([[1.0], [0.0], [1.0]])
+    u, t = x @ a.T * on, dy @ b * on
+    # sums of K fp32 products: K U of their terms off at most, twice in a row
+    off_u, off_t = (cols + 8) * U * (np.abs(x) @ np.abs(a).T), (rows + 8) * U * (np.abs(dy) @ np.abs(b))
+    want = fixed(X.numpy()) @ W.T + u @ b.T
+    close(Y, want, 4 * U * (np.abs(fixed(X.numpy())) @ np.abs(W).T + np.abs(want)) + off_u @ np.abs(b).T + (rank + 8) * U * (np.abs(u) @ np.abs(b).T), "Y")
+    close(dX, dy @ W + t @ a, grad_tolerance(dy, W, 16) + off_t @ np.abs(a) + (rank + 8) * U * (np.abs(t) @ np.abs(a) + np.abs(dy @ W)), "dX")
+    close(dA[-1], t.T @ x, off_t.T @ np.abs(x) + 8 * U * (np.abs(t).T @ np.abs(x)), "dA")
+    close(dB[-1], dy.T @ u, np.abs(dy).T @ off_u + 8 * U * (np.abs(dy).T @ np.abs(u)), "dB")
+    assert not dA[:-1].any() and not dB[:-1].any()
+
+
+@pytest.mark.gpu
+def test_batches_beyond_32_bits(pb):
+    """4096 vectors of 530000 rows: 2.2e9 values of dY, Y and the pre-activations."""
+    rows, cols, n, some = 530000, 32, 4096, [0, 1, 4095]
+    torch.manual_seed(5)
+    for layout in ("bits", "gates"):
+        layer = Layer(pb, rows, cols, 1, LAYOUTS[layout])
+        W = layer.matrix(1)
+        dY, X = torch.randn((n, rows), device="cuda"), torch.randn((n, cols), device="cuda")
+        x = fixed(X[some].cpu().numpy())
+        d64 = dY[some].double().cpu().numpy()
+        # (three digits: half a unit is 2^-23 of the largest value)
+        tolerance = 2.0 ** -23 / 0.998 * np.abs(d64).max(axis=1, keepdims=True) * np.abs(W).sum(axis=0) + 2 * 64 * U * (np.abs(d64) @ np.abs(W))
+        close(layer.lin.grad(dY)[some], d64 @ W, tolerance, "dX")
+        y = x @ W.T
+        if layout == "bits":
+            adapters = pb.Adapters(torch.zeros((2, 3, cols), device="cuda"), torch.randn((2, rows, 3), device="cuda"))
+            Y = layer.lin.adapted(X, adapters, torch.ones(n, dtype=torch.int32, device="cuda"))
+            close(Y[some], y, 4 * U * np.abs(y) + 1e-30, "Y")
+            dX, dA, dB = layer.lin.adapted_grad(X, dY, adapters, None)
+            close(dX[some], d64 @ W, tolerance, "dX")
+            assert dA[0].any() and not dA[1].any() and not dB.any()
+            del Y, dX, dA, dB, adapters
+        H, pre = layer.lin.gated(X, pb.PB_GATE_RELU, keep=True)
+        close(pre[some], y, 4 * U * np.abs(y) + 1e-30, "pre")
+        want = np.maximum(y[:, :rows // 2], 0) * y[:, rows // 2:]
+        close(H[some], want, 16 * U * np.abs(want) + 1e-30, "H")
+        del dY
+        dX, dpre = layer.lin.gated_grad(pre, torch.ones_like(H), pb.PB_GATE_RELU)
+        p = pre[some].double().cpu().numpy()
+        want = np.concatenate([p[:, rows // 2:] * (p[:, :rows // 2] > 0), np.maximum(p[:, :rows // 2], 0)], axis=1)
+        close(dpre[some], want, 4 * U * np.abs(want), "dpre")
+        tolerance = 2.0 ** -23 / 0.998 * np.abs(want).max(axis=1, keepdims=True) * np.abs(W).sum(axis=0) + 2 * 64 * U * (np.abs(want) @ np.abs(W))
+        close(dX[some], want @ W, tolerance, "dX")
+        del H, pre, dX, dpre
+        torch.cuda.empty_cache()
+
+
+class Everything:
+    """Every operator on the same layers, n vectors."""
+
+    def __init__(self, pb, n):
+        self.ffn, self.lin = Layer(pb, 360, 520, 8, LAYOUTS["gates"]).lin, Layer(pb, 333, 520, 8).lin
+        torch.manual_seed(n)
+        self.X, self.dY, self.dH = (torch.randn((n, k), device="cuda") for k in (520, 333, 180))
+        self.adapters = pb.Adapters(*(torch.randn(s, device="cuda").half() for s in ((3, 11, 520), (3, 333, 11))))
+        self.index = torch.randint(-1, 3, (n,), device="cuda", dtype=torch.int32)
+
+    def __call__(self):
+        H, pre = self.ffn.gated(self.X, keep=True)
+        return [H, pre, *self.ffn.gated_grad(pre, self.dH), self.lin.grad(self.dY), self.lin.adapted(self.X, self.adapters, self.index),
+                *self.lin.adapted_grad(self.X, self.dY, self.adapters, self.index)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 5, 40, 300])
+def test_captured_operators_follow_their_inputs(pb, n):
+    every = Everything(pb, n)
+    every()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = every()
+    for i in range(4):
+        for t in (every.X, every.dY, every.dH):
+            t.mul_(-0.75).add_(0.01 * i)
+        every.index.copy_(torch.roll(every.index, 1) if n > 1 else every.index * 0 + i - 1)
+        eager = every()
+        graph.replay()
+        torch.cuda.synchronize()
+        for g, e in zip(captured, eager):
+            assert torch.equal(g, e)
+
+
+@pytest.mark.gpu
+def test_threads_share_layers(pb):
+    """Four threads on streams of their own with the same layers and adapters."""
+    import threading
+    sets = [Everything(pb, n) for n in (1, 7, 40, 300)]
+    for s in sets[1:]:
+        s.ffn, s.lin, s.adapters = sets[0].ffn, sets[0].lin, sets[0].adapters
+    want = [s() for s in sets]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(s, w):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(10):
+                    got = s()
+                    stream.synchronize()
+                    if not all(torch.equal(g, e) for g, e in zip(got, w)):
+                        wrong.append(len(s.X))
+        except Exception as error:
+            wrong.append(error)
+    threads = [threading.Thread(target=work, args=a) for a in zip(sets, want)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not wrong, wrong
