@@ -234,6 +234,56 @@ __global__ __launch_bounds__(SCALES ? 1024 : 256) void k_grad_digits(const float
         if (d < 3 || !narrow) dst[64 * d] = out[d];
 }
 
+// The same rows of [dg; du] = [dH u act'(g); dH act(g)] on the gate layout, from the pre-activations [g; u] and dH of the vector: a tile has the gates and
+// the values of its units.  They go to `dpre` too, if that is given.
+__device__ __forceinline__ void gated_rows_of_step(const float *pre, const float *dh, float *dpre, int gate, int step, int lane, int gate_h, float (&v)[16])
+{
+    const int first = (step * 4 + (lane >> 4)) * 4;
+    float4_at4 x[4], h[2], out[4];      // x: gates of units first .. + 3 and gate_h + first .. + 3, then their values
+    auto load = [&](const float *at, auto whole) {
+        float4_at4 r;
+        if constexpr (decltype(whole)::value) {
+            r = *reinterpret_cast<const float4_at4 *>(at + first);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float one = at[min(first + i, gate_h - 1)];
+                r[i] = first + i < gate_h ? one : 0.0f;
+            }
+        }
+        return r;
+    };
+    auto load_all = [&](auto whole) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = load(pre + (size_t)k * gate_h, whole);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) h[k] = load(dh + (size_t)k * gate_h, whole);
+    };
+    if ((step * 4 + 4) * 4 <= gate_h) load_all(std::integral_constant<bool, true>());
+    else load_all(std::integral_constant<bool, false>());
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float act, slope;
+            gate_with_slope(gate, x[k][i], &act, &slope);
+            v[4 * i + k] = out[k][i] = h[k][i] * x[2 + k][i] * slope;
+            v[4 * i + 2 + k] = out[2 + k][i] = h[k][i] * act;
+        }
+    if (!dpre) return;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        float *const at = dpre + (size_t)k * gate_h + first;
+        if (first + 4 <= gate_h) {
+            *reinterpret_cast<float4_at4 *>(at) = out[k];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (first + i < gate_h) at[i] = out[k][i];
+        }
+    }
+}
+
 struct GradArgs {
     const uint32_t *packed;
     uint32_t packed_bytes, layer_step, round_step;   // (as in I8Args)
@@ -247,6 +297,7 @@ struct GradArgs {
     const float *dY;                                 // (FUSED)
     int rows, gate_h, held;                          // held: vectors in LDS, 4, 8 or 16
     int blocks, rows_of, workgroups;                 // column blocks, groups of vectors
+    GatedSource gated;                               // (GATED)
 
     // What workgroup `id` does.  Workgroups go round the eight XCDs, each with an L2 of its own: those of an XCD (id % 8) take a contiguous range of an
     // order in which eight column blocks (two to a line of weights) and then the vectors are next to each other, and read less of both.
@@ -281,10 +332,14 @@ struct GradShape {
 // FUSED: the workgroup scales the gradients of its rows by their own largest and keeps their digits in LDS, behind the codes.
 constexpr int kFusedSteps = 28;           // of four vectors; of eight half of them, of sixteen a quarter
 constexpr int kFusedLds = kFusedSteps * 1024;
-template <int Q, bool IL, int WM, bool FUSED>
+// GATED: these gradients are those of the pre-activations of a gated block on the gate layout, worked out here; every wave has one step at most, and
+// the workgroups of the first columns leave them in memory.  us, with k_gated_grad before it / inside: 5460 x 1000, 4 bitlayers, 40 vectors 18.1 / 16.3;
+// 5460 x 1024, 8 bitlayers, one vector 14.3 / 12.2, 16 vectors 17.2 / 16.0.
+constexpr int kGatedSteps = 8;
+template <int Q, bool IL, int WM, bool FUSED, bool GATED = false>
 __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
 {
-    static_assert(!FUSED || WM == 1);
+    static_assert((!FUSED || WM == 1) && (!GATED || FUSED));
     using S = GradShape<WM>;
     constexpr int WN = S::WN, NT = S::NT, TILES = S::TILES, KS = S::KS, TILE = S::TILE, BUF = TILES * TILE;
     extern __shared__ __align__(16) unsigned char s_codes[];
@@ -304,9 +359,16 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
     const int m = a.m;
 
     // (FUSED) the values of the wave's first step, which stay in registers
-    const float *const y = FUSED ? a.dY + (size_t)min(group * kGroupVectors + j, a.batch - 1) * a.rows : nullptr;
+    const float *const y = FUSED && !GATED ? a.dY + (size_t)min(group * kGroupVectors + j, a.batch - 1) * a.rows : nullptr;
     float held[16];
-    if constexpr (FUSED) rows_of_step(y, min(step0 + wave, step1 - 1), lane, a.rows, a.gate_h, held);
+    if constexpr (GATED) {
+        const size_t n = (size_t)min(group * kGroupVectors + j, a.batch - 1);
+        const bool writes = block == 0 && step0 + wave < step1 && group * kGroupVectors + j < a.batch;
+        gated_rows_of_step(a.gated.pre + n * a.rows, a.gated.dH + n * (a.rows / 2), writes ? a.gated.dpre + n * a.rows : nullptr, a.gated.gate,
+                           min(step0 + wave, step1 - 1), lane, a.gate_h, held);
+    } else if constexpr (FUSED) {
+        rows_of_step(y, min(step0 + wave, step1 - 1), lane, a.rows, a.gate_h, held);
+    }
 
     // the scales: whether they halve (as in k_i8_tile)
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(a.scales), 0, m * 4, 0x00020000);
@@ -333,11 +395,13 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
         uint32_t most = 0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) most = max(most, __float_as_uint(held[i]) & 0x7FFFFFFFu);
+        if constexpr (!GATED) {
 #pragma unroll 1
-        for (int s = step0 + wave + 8; s < step1; s += 8) {
-            rows_of_step(y, s, lane, a.rows, a.gate_h, v);
+            for (int s = step0 + wave + 8; s < step1; s += 8) {
+                rows_of_step(y, s, lane, a.rows, a.gate_h, v);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+                for (int i = 0; i < 16; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+            }
         }
         most = max(most, (uint32_t)__shfl_xor((int)most, 16));
         most = max(most, (uint32_t)__shfl_xor((int)most, 32));
@@ -349,7 +413,7 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
         if (threadIdx.x < 16) s_exponents[threadIdx.x] = e;
 #pragma unroll 1
         for (int s = wave; s < step1 - step0; s += 8) {
-            if (s >= 8) rows_of_step(y, step0 + s, lane, a.rows, a.gate_h, held);
+            if (!GATED && s >= 8) rows_of_step(y, step0 + s, lane, a.rows, a.gate_h, held);
             u32x4 out[4];
             digits_of(held, e, 0x808080, out);
             if (j < a.held) {
@@ -622,8 +686,10 @@ size_t grad_workspace_bytes(const Layout &L, int batch) { return grad_plan(L, ba
 
 #define PB_GRAD(WM, FUSED) {{reinterpret_cast<const void *>(k_grad<1, false, WM, FUSED>), reinterpret_cast<const void *>(k_grad<1, true, WM, FUSED>)}, \
                             {reinterpret_cast<const void *>(k_grad<2, false, WM, FUSED>), reinterpret_cast<const void *>(k_grad<2, true, WM, FUSED>)}}
-static const void *const kGradFn[4][2][2] = {PB_GRAD(1, false), PB_GRAD(4, false), PB_GRAD(8, false), PB_GRAD(1, true)};
-constexpr int kGradLds[4] = {GradShape<1>::LDS, GradShape<4>::LDS, GradShape<8>::LDS, GradShape<1>::LDS + kFusedLds};
+static const void *const kGradFn[5][2][2] = {PB_GRAD(1, false), PB_GRAD(4, false), PB_GRAD(8, false), PB_GRAD(1, true),
+                                             {{reinterpret_cast<const void *>(k_grad<1, false, 1, true, true>), nullptr},
+                                              {reinterpret_cast<const void *>(k_grad<2, false, 1, true, true>), nullptr}}};
+constexpr int kGradLds[5] = {GradShape<1>::LDS, GradShape<4>::LDS, GradShape<8>::LDS, GradShape<1>::LDS + kFusedLds, GradShape<1>::LDS + kFusedLds};
 
 int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, int bits_used, const float *dY, const GatedSource *gated,
                 int batch, float *dX, void *workspace, hipStream_t st)
@@ -636,12 +702,13 @@ int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, in
     // 2000 x 2000, 1000 vectors 35.6 / 38.2; 4096 columns, 1000 rows, 1000 vectors 27.2 / 29.7; 2048 x 2048, 256 vectors 24.4 / 24.2; but 1800 columns, 4100
     // rows, 104 vectors (262 KB) 24.4 / 23.2; 4096 x 4096, 64 vectors (262 KB) 29.2 / 28.4.
     const bool own = !gated && !p.held && (long long)(batch < 16 ? batch : 16) * L.rows <= 32768;
+    const bool gated_inside = gated && p.held && L.gate_h && p.steps_per_split <= kGatedSteps;
     int err = 0;
-    if (gated) {
+    if (gated && !gated_inside) {
         hipLaunchKernelGGL(k_gated_grad, dim3((unsigned)batch), dim3(1024), 0, st, gated->pre, gated->dH, L.rows / 2, gated->gate, gated->dpre,
                            scalings);
         dY = gated->dpre;
-    } else if (!own && !p.held) {
+    } else if (!gated && !own && !p.held) {
         hipLaunchKernelGGL(k_grad_scalings, dim3((unsigned)batch), dim3(1024), 0, st, dY, L.rows, scalings);
     }
     err = (int)hipGetLastError();
@@ -666,9 +733,10 @@ int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, in
     a.workgroups = a.blocks * a.rows_of * p.splits;
     float *const parts = reinterpret_cast<float *>(ws + p.parts_off);
     a.out = p.splits > 1 ? parts : dX;
-    const int shape = p.held ? 3 : (p.wm == 8 ? 2 : p.wm / 4), wide = bits_used > 4, il = is_pairs(L.layout);
+    if (gated) a.gated = *gated;
+    const int shape = gated_inside ? 4 : p.held ? 3 : (p.wm == 8 ? 2 : p.wm / 4), wide = bits_used > 4, il = is_pairs(L.layout);
     const void *fn = kGradFn[shape][wide][il];
-    static bool declared[4][2][2];      // (more than the default 64 KB of LDS)
+    static bool declared[5][2][2];      // (more than the default 64 KB of LDS)
     hipError_t e = hipSuccess;
     if (!__atomic_load_n(&declared[shape][wide][il], __ATOMIC_RELAXED)) {
         e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kGradLds[shape]);
