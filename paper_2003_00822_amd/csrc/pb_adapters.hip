@@ -17,7 +17,7 @@
 
 #include <type_traits>
 
-#include "pb_kernels.h"
+#include "pb_imma.h"
 
 namespace pb {
 
@@ -253,11 +253,11 @@ constexpr int kMany = 32, kPartsOfMany = 8;       // of more than 32 vectors (an
 __host__ __device__ constexpr int down_parts(int slices) { return slices > 4 ? slices : 4; }
 constexpr int kDownWaves = 8;
 template <typename T, bool TURNED, int RT>
-__device__ __forceinline__ void adapter_down(const DownArgs &a, int own, v4f (*s_part)[RT][64])
+__device__ __forceinline__ void adapter_down(const DownArgs &a, int item, int part, int own, v4f (*s_part)[RT][64])
 {
     const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Order::Tile it;
-    if (!a.order.tile(blockIdx.x, lane, &it)) return;
+    if (!a.order.tile(item, lane, &it)) return;
     const T *const M = static_cast<const T *>(a.M) + (size_t)it.adapter * a.rank * a.length;
     const float *const x = a.V + (size_t)it.vector * a.length;
     // (RT tiles that there are, also where this workgroup's own are fewer: all but the last are whole)
@@ -300,7 +300,7 @@ __device__ __forceinline__ void adapter_down(const DownArgs &a, int own, v4f (*s
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[t] = mfma(w[q][t][e], v[q][e], acc[t]);
     };
-    for (int c0 = (blockIdx.y * kDownWaves + wave) * 64; c0 < a.length; c0 += a.slices * kDownWaves * 64) {
+    for (int c0 = (part * kDownWaves + wave) * 64; c0 < a.length; c0 += a.slices * kDownWaves * 64) {
         if (c0 + 64 <= a.length) {
             step(c0, yes(), std::integral_constant<int, 4>());
         } else {
@@ -327,7 +327,7 @@ __device__ __forceinline__ void adapter_down(const DownArgs &a, int own, v4f (*s
         for (int e = 0; e < 4; ++e)
             if ((rt0 + t) * 16 + 4 * kb + e >= a.rank) v[e] = 0.0f;
         const int parts = down_parts(a.slices), own_parts = parts / a.slices;
-        float *const out = a.out + (((size_t)it.vector * a.ranks + rt0 + t) * 16 + 4 * kb) * parts + blockIdx.y * own_parts;
+        float *const out = a.out + (((size_t)it.vector * a.ranks + rt0 + t) * 16 + 4 * kb) * parts + part * own_parts;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (own_parts == 4) *reinterpret_cast<v4f *>(out + e * parts) = v4f{v[e], 0, 0, 0};
@@ -342,8 +342,29 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_adapter_down(const DownArgs
 {
     __shared__ v4f s_part[kDownWaves - 1][RT][64];
     const int z = blockIdx.z * RT;
-    if (u.V && z < u.ranks) adapter_down<T, false, RT>(u, z, s_part);
-    else adapter_down<T, true, RT>(t, u.V ? z - (u.ranks + RT - 1) / RT * RT : z, s_part);
+    if (u.V && z < u.ranks) adapter_down<T, false, RT>(u, blockIdx.x, blockIdx.y, z, s_part);
+    else adapter_down<T, true, RT>(t, blockIdx.x, blockIdx.y, u.V ? z - (u.ranks + RT - 1) / RT * RT : z, s_part);
+}
+// u beside the activations' digits, both of which only read x: the first workgroups do four units of the digits each
+struct DigitsJob {
+    ActSource act;
+    uint8_t *digits, *wide;
+    uint32_t turn;
+    int cq, units, workgroups;
+};
+template <typename T, int RT>
+__global__ __launch_bounds__(kDownWaves * 64) void k_adapter_down_x(const DownArgs u, const DigitsJob job, const int items)
+{
+    __shared__ v4f s_part[kDownWaves - 1][RT][64];
+    __shared__ int s_wide[kDownWaves];
+    const int id = blockIdx.x;
+    if (id < job.workgroups) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), unit = min(id * (kDownWaves / 2) + wave / 2, job.units - 1);
+        digits_unit<4>(job.act, job.cq, job.digits, job.wide, nullptr, job.turn, unit % job.cq, unit / job.cq, wave & 1, s_wide + (wave & ~1));
+    } else {
+        const int at = id - job.workgroups, rest = at / items;
+        adapter_down<T, false, RT>(u, at % items, rest % u.slices, rest / u.slices * RT, s_part);
+    }
 }
 // Rank i of rank tile `rt` of a vector: the parts added up in a fixed order
 template <int PARTS>
@@ -693,6 +714,34 @@ int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layou
                                           reinterpret_cast<const void *>(k_adapter_down<T, 3>), reinterpret_cast<const void *>(k_adapter_down<T, 4>)};
         return launch(fn[rt - 1], dim3((unsigned)p.items, (unsigned)p.slices, (unsigned)(z * ((X ? 1 : 0) + (dY ? 1 : 0)))), kDownWaves * 64, &u, &t,
                       nullptr, st);
+    });
+}
+
+int launch_adapter_down_digits(AdapterDown *d, const ActSource &act, int cq, void *digits, void *wide, bool plain, hipStream_t st)
+{
+    const AdapterPlan &p = *d->plan;
+    const pb_adapters &ad = *d->adapters;
+    const int rt = rank_tiles(p.ranks), z = (p.ranks + rt - 1) / rt;
+    DownArgs u;
+    u.order = order_of(p, ad, d->index, act.batch, d->workspace);
+    u.M = ad.A; u.scale = nullptr; u.V = d->X;
+    u.out = reinterpret_cast<float *>(static_cast<char *>(d->workspace) + p.u_off);
+    u.length = d->layout->cols; u.rank = ad.rank; u.ranks = p.ranks; u.slices = p.slices;
+    DigitsJob job;
+    job.act = act;
+    job.digits = static_cast<uint8_t *>(digits);
+    job.wide = static_cast<uint8_t *>(wide);
+    job.turn = plain ? 0x80808080u : 0u;
+    job.cq = cq;
+    job.units = cq * ((act.batch + 3) / 4);
+    job.workgroups = (job.units + kDownWaves / 2 - 1) / (kDownWaves / 2);
+    int items = p.items;
+    d->done = true;
+    return by_type(ad.type, [&](auto type) {
+        typedef decltype(type) T;
+        static const void *const fn[4] = {reinterpret_cast<const void *>(k_adapter_down_x<T, 1>), reinterpret_cast<const void *>(k_adapter_down_x<T, 2>),
+                                          reinterpret_cast<const void *>(k_adapter_down_x<T, 3>), reinterpret_cast<const void *>(k_adapter_down_x<T, 4>)};
+        return launch(fn[rt - 1], dim3((unsigned)(job.workgroups + p.items * p.slices * z)), kDownWaves * 64, &u, &job, &items, st);
     });
 }
 

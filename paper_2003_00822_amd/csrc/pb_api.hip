@@ -469,17 +469,25 @@ int pb_matmul_adapters(const void *packed, const float *scales, const pb_desc *d
     const pb::AdapterPlan p = pb::adapter_plan(L, *adapters, batch, index != nullptr);
     void *const ws = static_cast<char *>(workspace) + adapters_off(L, batch);
     int err = pb::launch_adapter_order(p, *adapters, index, batch, ws, st);
-    if (!err) err = pb::launch_adapter_down(p, *adapters, L, index, X, nullptr, batch, ws, st);
     if (err) return hip_status(err);
+    pb::AdapterDown down = {&p, adapters, &L, index, X, ws, false};
     pb::Epilogue ep;
     ep.bias = bias;
     ep.pre = reinterpret_cast<float *>(static_cast<char *>(workspace) + pb::ws_gates_off(L, batch));
     // (one vector: B_k u behind the product, a launch less)
     const pb::AdapterRows rows = pb::adapter_rows(p, *adapters, index, ws);
     const bool behind = batch == 1 && pb::is_tile16(L.layout) && !pb::takes_digits(L, batch) && adapters->rank <= pb::kAdapterRowsRank;
-    if (behind) ep.adapter = &rows;
+    if (behind) {
+        ep.adapter = &rows;
+        err = pb::launch_adapter_down(p, *adapters, L, index, X, nullptr, batch, ws, st);
+        if (err) return hip_status(err);
+    } else {
+        ep.down = &down;
+    }
     rc = matmul_common(packed, scales, d, bits_used, X, d->cols, nullptr, 0, batch, Y, nullptr, workspace, stream, ep, false, true);
     if (rc != PB_OK || behind) return rc;
+    if (!down.done) err = pb::launch_adapter_down(p, *adapters, L, index, X, nullptr, batch, ws, st);
+    if (err) return hip_status(err);
     return hip_status(pb::launch_adapter_up(p, *adapters, L, index, batch, Y, ws, st));
 }
 

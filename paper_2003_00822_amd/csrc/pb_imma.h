@@ -231,6 +231,50 @@ __device__ __forceinline__ uint32_t digits_at(int group, int vectors, int cq, in
            (uint32_t)(quad * nd * 64 + ((digit * 4 + kb) * in_quad + (v & 3)) * 16);
 }
 
+// The activations as byte digits in memory, for the calls that read them more than once: chunk q of the four vectors `quad`, by two waves, each the
+// words t, t + 1 (mod 4).  The lanes are in the order in which the
+// digits lie in memory: the order of the activations, two lanes to a word, took 0.2 us longer (56 vectors, 1402 columns).
+// `turn`: what makes u of the third byte's u ^ 0x80.  The workgroup meets at a barrier.
+template <int ND>
+__device__ __forceinline__ void digits_unit(const ActSource &s, int cq, uint8_t *__restrict__ digits, uint8_t *__restrict__ wide,
+                                            int32_t *__restrict__ xq_out, const uint32_t turn, const int q, const int quad, const int wave, int *s_wide)
+{
+    const int lane = threadIdx.x & 63, group = quad * 4 / kGroupVectors;
+    const int kb = (lane >> 2) & 3, th = 4 * wave + (lane >> 4), n = 4 * quad + (lane & 3);
+    const int vec = n % kGroupVectors, vectors = group_vectors(s.batch, group);
+    const int c = 512 * q + 32 * (4 * kb + th / 2) + 4 * (th % 2);
+    u32x4 v[4];
+    load_columns(s, n, c, 512 * (q + 1), v);
+    convert_columns(s, v);
+    if (xq_out && n < s.batch) {
+        const int cols = s.cols0 + s.cols1;
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (c + 8 * b + r < cols) xq_out[(size_t)n * cols + c + 8 * b + r] = (int32_t)v[b][r];
+    }
+    u32x4 out[ND];
+    byte_digits<ND>(v, out);
+    if constexpr (ND == 4) out[2] ^= turn;
+    if (vec < vectors) {
+        uint8_t *dst = digits + (size_t)(q * 8 + th) * digits_step(vectors, ND);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) *reinterpret_cast<u32x4 *>(dst + digits_at(group, vectors, cq, ND, d, kb, vec)) = out[d];
+    }
+    if constexpr (ND == 4) {
+        uint32_t high = 0;   // bits that differ from the sign
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) high |= v[b][r] ^ (uint32_t)((int32_t)v[b][r] >> 31);
+        const bool any = __builtin_amdgcn_ballot_w64(high >> 23 != 0) != 0;
+        if (lane == 0) s_wide[wave] = any;
+        __syncthreads();
+        if (wave == 0 && lane == 0) wide[quad * 64 + q] = (uint8_t)(s_wide[0] | s_wide[1]);
+    }
+}
+
 struct I8Args {
     const uint32_t *packed;
     uint32_t packed_bytes;               // (below 2^32)

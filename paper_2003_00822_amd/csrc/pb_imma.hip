@@ -7,50 +7,12 @@
 
 namespace pb {
 
-// The activations as byte digits in memory, for the calls that read them more than once (pb_imma.h has the order).
-// A workgroup does one chunk of four vectors, each of its two waves the words t, t + 1 (mod 4).  The lanes are in the order in which the
-// digits lie in memory: the order of the activations, two lanes to a word, took 0.2 us longer (56 vectors, 1402 columns).
-// `turn`: what makes u of the third byte's u ^ 0x80.
 template <int ND>
 __global__ __launch_bounds__(128) void k_digits(ActSource s, int cq, uint8_t *__restrict__ digits, uint8_t *__restrict__ wide,
                                                 int32_t *__restrict__ xq_out, const uint32_t turn)
 {
     __shared__ int s_wide[2];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int q = blockIdx.x, quad = blockIdx.y, group = quad * 4 / kGroupVectors;
-    const int kb = (lane >> 2) & 3, th = 4 * wave + (lane >> 4), n = 4 * quad + (lane & 3);
-    const int vec = n % kGroupVectors, vectors = group_vectors(s.batch, group);
-    const int c = 512 * q + 32 * (4 * kb + th / 2) + 4 * (th % 2);
-    u32x4 v[4];
-    load_columns(s, n, c, 512 * (q + 1), v);
-    convert_columns(s, v);
-    if (xq_out && n < s.batch) {
-        const int cols = s.cols0 + s.cols1;
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (c + 8 * b + r < cols) xq_out[(size_t)n * cols + c + 8 * b + r] = (int32_t)v[b][r];
-    }
-    u32x4 out[ND];
-    byte_digits<ND>(v, out);
-    if constexpr (ND == 4) out[2] ^= turn;
-    if (vec < vectors) {
-        uint8_t *dst = digits + (size_t)(q * 8 + th) * digits_step(vectors, ND);
-#pragma unroll
-        for (int d = 0; d < ND; ++d) *reinterpret_cast<u32x4 *>(dst + digits_at(group, vectors, cq, ND, d, kb, vec)) = out[d];
-    }
-    if constexpr (ND == 4) {
-        uint32_t high = 0;   // bits that differ from the sign
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) high |= v[b][r] ^ (uint32_t)((int32_t)v[b][r] >> 31);
-        const bool any = __builtin_amdgcn_ballot_w64(high >> 23 != 0) != 0;
-        if (lane == 0) s_wide[wave] = any;
-        __syncthreads();
-        if (threadIdx.x == 0) wide[quad * 64 + q] = (uint8_t)(s_wide[0] | s_wide[1]);
-    }
+    digits_unit<ND>(s, cq, digits, wide, xq_out, turn, blockIdx.x, blockIdx.y, threadIdx.x >> 6, s_wide);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -330,13 +292,19 @@ int launch_imma(const uint32_t *packed, const float *scales, const Layout &L, in
     int cus;
     const hipError_t no_device = compute_units(&cus);
     if (no_device != hipSuccess) return (int)no_device;
+    // The adapters' first products go along with the digits up to 16 MB of activations, which saves a launch.  us, together / one after the other: 4096
+    // columns, 48 vectors 25.1 / 27.4, 512 vectors 55.2 / 57.4; 768 columns, 2017 vectors 47.0 / 50.2; but 4096 columns, 2048 vectors (34 MB) 246.4 / 244.4.
+    auto make_digits = [&](bool plain) {
+        if (ep.down && nd == 4 && (long long)batch * L.cols <= 1 << 22) return launch_adapter_down_digits(ep.down, a.act, L.cq, digits, wide, plain, st);
+        return launch_digits(X0, cols0, X1, cols1, batch, L, frac_bits, act_bits, digits, wide, nullptr, plain, st);
+    };
     // Large batches of the operators: the kernel of pb_batch.hip where its workgroups, one per compute unit, fill 65 % of their rounds over the chip.
     // us with it / with the kernels below, 8 bitlayers, digits included: 8192 x 2048, 300 vectors (192 workgroups) 31.0 / 34.7; 24600 x 4096, 65
     // (193) 46.1 / 52.7; 16384 x 4096, 140 (256) 49.2 / 53.0; 2048 x 8192, 2048 (256) 111 / 138; 6000 x 600, 2000 (752) 60 / 95; but 2048 x 8192, 1000 (128)
     // 80 / 72, 4096 x 4096, 512 (128) 50 / 42, 12000 x 8192, 5 bitlayers, 100 (94) 71 / 51.
     const int large = ep.pre && nd == 4 && batch > 64 ? batch_workgroups(L.rt_count, batch) : 0;
     if (large * 20 >= (large + cus - 1) / cus * cus * 13 && large) {
-        const int e = launch_digits(X0, cols0, X1, cols1, batch, L, frac_bits, act_bits, digits, wide, nullptr, true, st);
+        const int e = make_digits(true);
         return e ? e : launch_imma_batch(a, il, ep.pre, st);
     }
     int way = pick_way(c, prepared, cus);
@@ -347,7 +315,7 @@ int launch_imma(const uint32_t *packed, const float *scales, const Layout &L, in
     if (way == kMemory1 && nd == 4 && (prepared || (c.tiles > 4 && bits_used <= 4 && !A && !ep.fused()))) way = kPlain1;
     const int shape = way - kStreams;
     if (!prepared && !is_fused(way)) {
-        const int e = launch_digits(X0, cols0, X1, cols1, batch, L, frac_bits, act_bits, digits, wide, nullptr, way != kMemory1, st);
+        const int e = make_digits(way != kMemory1);
         if (e) return e;
     }
     if (shape >= 0) {

@@ -36,6 +36,7 @@ struct AdapterRows {
     const int32_t *index;
     int rank, count, type, nparts;
 };
+struct AdapterDown;
 constexpr int kAdapterRowsRank = 16;     // (32 cost scratch memory in two of the kernels)
 struct Epilogue {
     const float *bias = nullptr;   // [rows] or null
@@ -44,6 +45,7 @@ struct Epilogue {
     float *h_out = nullptr, *c_out = nullptr;
     int gate = -1;                 // 0 or more: fused gated block (a pb_gate)
     float *pre = nullptr;          // non-null: room for [batch][rows], and the kernel for large batches of pb_batch.hip may be taken
+    AdapterDown *down = nullptr;   // adapters whose u = A_k x is wanted: where the activations' digits have a launch, it does both
     const AdapterRows *adapter = nullptr;   // (one vector, tiled layouts but the pairs')
     bool fused() const { return c_prev || gate >= 0; }
 };
@@ -105,6 +107,18 @@ int launch_adapter_order(const AdapterPlan &p, const pb_adapters &ad, const int3
 // u = A_k x (and t = scale_k B_k^T dY, if dY is given) of the ordered vectors, in parts
 int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, const float *X, const float *dY, int batch,
                         void *workspace, hipStream_t st);
+// The same for x beside k_digits<4> in one launch, which then is `done`
+struct AdapterDown {
+    const AdapterPlan *plan;
+    const pb_adapters *adapters;
+    const Layout *layout;
+    const int32_t *index;
+    const float *X;
+    void *workspace;
+    bool done;
+};
+struct ActSource;
+int launch_adapter_down_digits(AdapterDown *down, const ActSource &act, int cq, void *digits, void *wide, bool plain, hipStream_t st);
 // Y += scale_k B_k u; what launch_mfma needs to do it for one vector
 AdapterRows adapter_rows(const AdapterPlan &p, const pb_adapters &ad, const int32_t *index, void *workspace);
 int launch_adapter_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, int batch, float *Y, void *workspace,
