@@ -397,18 +397,17 @@ struct UpArgs {
 // A wave does `blocks` times 64 values of the tile's vectors.  RT rank tiles at once.  TURNED: M is A [rank][length], else B [length][rank].
 // Values behind the last are computed from others' rows or columns and not stored.
 constexpr int kUpRow = 20;        // floats per rank in LDS: the vectors of the tile, and room that puts neighbouring ranks on other banks
-template <typename T, bool TURNED, int RT>
-__global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
+template <typename T, bool TURNED, int RT, int WAVES>
+__device__ __forceinline__ void adapter_up(const UpArgs &a, int column, int item, float *s_u)
 {
     const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int first = (blockIdx.x * 4 + wave) * a.blocks * 64, end = min(first + a.blocks * 64, a.length);
-    __shared__ float s_u[PB_MAX_RANK * kUpRow];
+    const int first = (column * WAVES + wave) * a.blocks * 64, end = min(first + a.blocks * 64, a.length);
     Order::Tile it;
-    if (!a.order.tile(blockIdx.y, lane, &it)) return;
+    if (!a.order.tile(item, lane, &it)) return;
     const T *const M = static_cast<const T *>(a.M) + (size_t)it.adapter * a.rank * a.length;
     const float s = a.scale ? a.scale[it.adapter] : 1.0f;
-    // the parts of u (t) are added up once per workgroup: a thread has a rank of every rank tile of one vector
-    by_parts<16>(a.slices, [&](auto parts) {
+    // the parts of u (t) are added up once per workgroup: a thread of the first 256 has a rank of every rank tile of one vector
+    if (wave < 4) by_parts<16>(a.slices, [&](auto parts) {
         const int v = threadIdx.x / 16, vector = __shfl(it.vector, v);
         for (int rt0 = 0; rt0 < a.ranks; rt0 += RT) {
             float sum[RT];
@@ -497,6 +496,13 @@ __global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
     }
 }
 
+template <typename T, bool TURNED, int RT>
+__global__ __launch_bounds__(256) void k_adapter_up(const UpArgs a)
+{
+    __shared__ float s_u[PB_MAX_RANK * kUpRow];
+    adapter_up<T, TURNED, RT, 4>(a, blockIdx.x, blockIdx.y, s_u);
+}
+
 // ---- dA_k = sum t x^T, dB_k = scale_k sum dy u^T ----
 struct OuterArgs {
     Order order;
@@ -512,11 +518,11 @@ constexpr int outer_waves(bool split) { return split ? 16 : 4; }
 constexpr int kOuterVectors = 8;       // (not split) vectors whose ranks are in LDS at a time
 constexpr int outer_lds(bool split, int rt) { return split ? outer_waves(true) * rt * 4 * 64 * 4 : rt * 16 * kOuterVectors; }      // in floats
 template <bool TURNED, bool SPLIT, int RT>
-__device__ __forceinline__ void adapter_outer(const OuterArgs &a, int block, float *lds)
+__device__ __forceinline__ void adapter_outer(const OuterArgs &a, int block, int k, int own, float *lds)
 {
     constexpr int WAVES = SPLIT ? outer_waves(true) : 1;
     const int lane = threadIdx.x & 63, kb = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int k = blockIdx.y, rt0 = blockIdx.z * RT, c0 = (SPLIT ? block : block * outer_waves(false) + wave) * 64, c = c0 + 4 * i;
+    const int rt0 = own * RT, c0 = (SPLIT ? block : block * outer_waves(false) + wave) * 64, c = c0 + 4 * i;
     const Order::Segment seg = a.order.segment(k, lane);
     v4f acc[RT][4];
 #pragma unroll
@@ -617,8 +623,27 @@ __global__ __launch_bounds__(outer_waves(SPLIT) * 64) void k_adapter_outer(const
 {
     __shared__ __align__(16) float lds[outer_lds(SPLIT, RT)];
     const int block = blockIdx.x;
-    if (block < of_A) adapter_outer<false, SPLIT, RT>(A, block, lds);
-    else adapter_outer<true, SPLIT, RT>(B, block - of_A, lds);
+    if (block < of_A) adapter_outer<false, SPLIT, RT>(A, block, blockIdx.y, blockIdx.z, lds);
+    else adapter_outer<true, SPLIT, RT>(B, block - of_A, blockIdx.y, blockIdx.z, lds);
+}
+// dX += A_k^T t beside dA and dB, which do not need it: the first of_A + of_B workgroups per adapter and rank tiles do these.  us of the whole backward
+// pass, in two launches / in one: 1500 x 701, 3 of rank 9 in fp32, 100 vectors 32.6 / 28.6; 4096 x 4096, 4 of 16 in bf16, 2048 vectors 165 / 162.5;
+// 8698 x 6860, 36 of 42 in fp16, 25 vectors 70.5 / 67.2.
+struct OuterGrid { int of_A, blocks, count, workgroups, up_blocks; };
+template <typename T, bool SPLIT, int RT>
+__global__ __launch_bounds__(outer_waves(SPLIT) * 64) void k_adapter_grads(const OuterArgs A, const OuterArgs B, const UpArgs up, const OuterGrid g)
+{
+    constexpr int OUTER_RT = SPLIT && RT > 2 ? 2 : RT, LDS = outer_lds(SPLIT, OUTER_RT), UP = PB_MAX_RANK * kUpRow;
+    __shared__ __align__(16) float lds[LDS > UP ? LDS : UP];
+    const int id = blockIdx.x;
+    if (id >= g.workgroups) {
+        const int at = id - g.workgroups;
+        adapter_up<T, true, RT, outer_waves(SPLIT)>(up, at % g.up_blocks, at / g.up_blocks, lds);
+        return;
+    }
+    const int block = id % g.blocks, rest = id / g.blocks;
+    if (block < g.of_A) adapter_outer<false, SPLIT, OUTER_RT>(A, block, rest % g.count, rest / g.count, lds);
+    else adapter_outer<true, SPLIT, OUTER_RT>(B, block - g.of_A, rest % g.count, rest / g.count, lds);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -746,21 +771,26 @@ int launch_adapter_down_digits(AdapterDown *d, const ActSource &act, int cq, voi
 }
 
 // Y += ... with B (TURNED: dX += ... with A)
-template <bool TURNED>
-static int launch_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, int batch, float *out, void *workspace,
-                     hipStream_t st)
+static UpArgs up_args(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, int batch, float *out, void *workspace, bool turned)
 {
     UpArgs a;
     a.order = order_of(p, ad, index, batch, workspace);
-    a.M = TURNED ? ad.A : ad.B;
-    a.scale = TURNED ? nullptr : ad.scale;
-    a.parts = reinterpret_cast<const float *>(static_cast<char *>(workspace) + (TURNED ? p.t_off : p.u_off));
+    a.M = turned ? ad.A : ad.B;
+    a.scale = turned ? nullptr : ad.scale;
+    a.parts = reinterpret_cast<const float *>(static_cast<char *>(workspace) + (turned ? p.t_off : p.u_off));
     a.out = out;
-    a.length = TURNED ? L.cols : L.rows;
+    a.length = turned ? L.cols : L.rows;
     a.rank = ad.rank; a.ranks = p.ranks; a.slices = p.slices;
     // Blocks of 64 values per wave: one while that leaves the chip room, up to four (a wave finds its tile and its ranks once)
     const long long waves = (long long)((a.length + 63) / 64) * p.items;
     a.blocks = waves < 2 * 4096 ? 1 : (waves < 4 * 4096 ? 2 : 4);
+    return a;
+}
+template <bool TURNED>
+static int launch_up(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, int batch, float *out, void *workspace,
+                     hipStream_t st)
+{
+    UpArgs a = up_args(p, ad, L, index, batch, out, workspace, TURNED);
     const int rt = rank_tiles(p.ranks);
     return by_type(ad.type, [&](auto type) {
         typedef decltype(type) T;
@@ -786,11 +816,7 @@ int launch_adapter_grads(const AdapterPlan &p, const pb_adapters &ad, const Layo
                          float *dX, float *dA, float *dB, void *workspace, hipStream_t st)
 {
     char *const ws = static_cast<char *>(workspace);
-    if (dX) {
-        const int err = launch_up<true>(p, ad, L, index, batch, dX, workspace, st);
-        if (err) return err;
-    }
-    if (!dA && !dB) return 0;
+    if (!dA && !dB) return launch_up<true>(p, ad, L, index, batch, dX, workspace, st);
     OuterArgs A, B;
     A.order = order_of(p, ad, index, batch, workspace);
     A.rank = ad.rank; A.ranks = p.ranks; A.slices = p.slices;
@@ -811,8 +837,29 @@ int launch_adapter_grads(const AdapterPlan &p, const pb_adapters &ad, const Layo
                                           {reinterpret_cast<const void *>(k_adapter_outer<true, 1>), reinterpret_cast<const void *>(k_adapter_outer<true, 2>)}};
     int of_A = dA ? (L.cols + columns - 1) / columns : 0;
     const int of_B = dB ? (L.rows + columns - 1) / columns : 0;
-    return launch(fns[split][rt - 1], dim3((unsigned)(of_A + of_B), (unsigned)ad.count, (unsigned)((p.ranks + rt - 1) / rt)), outer_waves(split) * 64, &A,
-                  &B, &of_A, st);
+    const int z = (p.ranks + rt - 1) / rt;
+    UpArgs up = up_args(p, ad, L, index, batch, dX, workspace, true);
+    const int per = outer_waves(split) * 64 * up.blocks;
+    OuterGrid g = {of_A, of_A + of_B, ad.count, 0, (L.cols + per - 1) / per};
+    const long long workgroups = (long long)g.blocks * ad.count * z + (long long)g.up_blocks * p.items;
+    // (a dimension of a grid has fewer than 2^32 threads)
+    const bool together = dX && workgroups * outer_waves(split) * 64 < 1ll << 32;
+    if (dX && !together) {
+        const int err = launch_up<true>(p, ad, L, index, batch, dX, workspace, st);
+        if (err) return err;
+    }
+    if (!together) return launch(fns[split][rt - 1], dim3((unsigned)(of_A + of_B), (unsigned)ad.count, (unsigned)z), outer_waves(split) * 64, &A, &B, &of_A, st);
+    g.workgroups = g.blocks * ad.count * z;
+    return by_type(ad.type, [&](auto type) {
+        typedef decltype(type) T;
+#define PB_GRADS(SPLIT) {reinterpret_cast<const void *>(k_adapter_grads<T, SPLIT, 1>), reinterpret_cast<const void *>(k_adapter_grads<T, SPLIT, 2>), \
+                         reinterpret_cast<const void *>(k_adapter_grads<T, SPLIT, 3>), reinterpret_cast<const void *>(k_adapter_grads<T, SPLIT, 4>)}
+        static const void *const fn[2][4] = {PB_GRADS(false), PB_GRADS(true)};
+        void *list[] = {&A, &B, &up, &g};
+        const hipError_t e = hipLaunchKernel(fn[split][alone_rt - 1], dim3((unsigned)workgroups),
+                                             dim3((unsigned)outer_waves(split) * 64), list, 0, st);
+        return (int)(e != hipSuccess ? e : hipGetLastError());
+    });
 }
 
 }  // namespace pb
