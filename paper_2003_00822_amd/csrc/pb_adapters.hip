@@ -17,7 +17,7 @@
 
 #include <type_traits>
 
-#include "pb_imma.h"
+#include "pb_grad.h"
 
 namespace pb {
 
@@ -345,7 +345,24 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_adapter_down(const DownArgs
     if (u.V && z < u.ranks) adapter_down<T, false, RT>(u, blockIdx.x, blockIdx.y, z, s_part);
     else adapter_down<T, true, RT>(t, blockIdx.x, blockIdx.y, u.V ? z - (u.ranks + RT - 1) / RT * RT : z, s_part);
 }
-// u beside the activations' digits, both of which only read x: the first workgroups do four units of the digits each
+// u, t or both beside the scalings of dY, which the last workgroups do, a vector each.  us of the backward pass, together / one after the other:
+// 4096 x 4096, 4 of rank 16 in bf16, 2048 vectors 161.7 / 168.1; 8582 x 935, 5 of 50 in fp16, 670 vectors 105.5 / 111.9; 4096 x 4096, one of 16, 48 vectors
+// 35 / 38.  (With the scalings first, which are short, 164.4, 109.7, 35.)
+template <typename T, int RT>
+__global__ __launch_bounds__(kDownWaves * 64) void k_adapter_down_dy(const DownArgs u, const DownArgs t, const float *__restrict__ dY, int rows,
+                                                                     Scaling *__restrict__ scalings, int batch, int items)
+{
+    __shared__ v4f s_part[kDownWaves - 1][RT][64];
+    const int at = blockIdx.x, scales = gridDim.x - batch;
+    if (at >= scales) {
+        scale_vector<kDownWaves>(dY, rows, at - scales, scalings);
+        return;
+    }
+    const int rest = at / items, item = at % items, part = rest % u.slices, z = rest / u.slices * RT;
+    if (u.V && z < u.ranks) adapter_down<T, false, RT>(u, item, part, z, s_part);
+    else adapter_down<T, true, RT>(t, item, part, u.V ? z - (u.ranks + RT - 1) / RT * RT : z, s_part);
+}
+// u beside the activations' digits, both of which only read x: the last workgroups do four units of the digits each
 struct DigitsJob {
     ActSource act;
     uint8_t *digits, *wide;
@@ -357,12 +374,11 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_adapter_down_x(const DownAr
 {
     __shared__ v4f s_part[kDownWaves - 1][RT][64];
     __shared__ int s_wide[kDownWaves];
-    const int id = blockIdx.x;
-    if (id < job.workgroups) {
+    const int at = blockIdx.x, rest = at / items, id = at - (int)(gridDim.x - job.workgroups);
+    if (id >= 0) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), unit = min(id * (kDownWaves / 2) + wave / 2, job.units - 1);
         digits_unit<4>(job.act, job.cq, job.digits, job.wide, nullptr, job.turn, unit % job.cq, unit / job.cq, wave & 1, s_wide + (wave & ~1));
     } else {
-        const int at = id - job.workgroups, rest = at / items;
         adapter_down<T, false, RT>(u, at % items, rest % u.slices, rest / u.slices * RT, s_part);
     }
 }
@@ -722,17 +738,22 @@ static int launch(const void *fn, dim3 grid, int threads, void *first, void *sec
     return (int)(e != hipSuccess ? e : hipGetLastError());
 }
 
+static void down_args(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, const float *X, const float *dY, int batch,
+                      void *workspace, DownArgs *u, DownArgs *t)
+{
+    char *const ws = static_cast<char *>(workspace);
+    u->order = order_of(p, ad, index, batch, workspace);
+    u->rank = ad.rank; u->ranks = p.ranks; u->slices = p.slices;
+    *t = *u;
+    u->M = ad.A; u->scale = nullptr; u->V = X; u->length = L.cols; u->out = reinterpret_cast<float *>(ws + p.u_off);
+    t->M = ad.B; t->scale = ad.scale; t->V = dY; t->length = L.rows; t->out = reinterpret_cast<float *>(ws + p.t_off);
+}
 int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, const float *X, const float *dY, int batch,
                         void *workspace, hipStream_t st)
 {
-    char *const ws = static_cast<char *>(workspace);
     const int rt = rank_tiles(p.ranks), z = (p.ranks + rt - 1) / rt;
     DownArgs u, t;
-    u.order = order_of(p, ad, index, batch, workspace);
-    u.rank = ad.rank; u.ranks = p.ranks; u.slices = p.slices;
-    t = u;
-    u.M = ad.A; u.scale = nullptr; u.V = X; u.length = L.cols; u.out = reinterpret_cast<float *>(ws + p.u_off);
-    t.M = ad.B; t.scale = ad.scale; t.V = dY; t.length = L.rows; t.out = reinterpret_cast<float *>(ws + p.t_off);
+    down_args(p, ad, L, index, X, dY, batch, workspace, &u, &t);
     return by_type(ad.type, [&](auto type) {
         typedef decltype(type) T;
         static const void *const fn[4] = {reinterpret_cast<const void *>(k_adapter_down<T, 1>), reinterpret_cast<const void *>(k_adapter_down<T, 2>),
@@ -742,16 +763,31 @@ int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layou
     });
 }
 
+int launch_adapter_down_scalings(AdapterDown *d, const float *dY, int batch, Scaling *scalings, hipStream_t st)
+{
+    const AdapterPlan &p = *d->plan;
+    const pb_adapters &ad = *d->adapters;
+    const int rt = rank_tiles(p.ranks), z = (p.ranks + rt - 1) / rt * ((d->X ? 1 : 0) + (d->dY ? 1 : 0));
+    DownArgs u, t;
+    down_args(p, ad, *d->layout, d->index, d->X, d->dY, batch, d->workspace, &u, &t);
+    int rows = d->layout->rows, items = p.items;
+    d->done = true;
+    return by_type(ad.type, [&](auto type) {
+        typedef decltype(type) T;
+        static const void *const fn[4] = {reinterpret_cast<const void *>(k_adapter_down_dy<T, 1>), reinterpret_cast<const void *>(k_adapter_down_dy<T, 2>),
+                                          reinterpret_cast<const void *>(k_adapter_down_dy<T, 3>), reinterpret_cast<const void *>(k_adapter_down_dy<T, 4>)};
+        void *list[] = {&u, &t, &dY, &rows, &scalings, &batch, &items};
+        const hipError_t e = hipLaunchKernel(fn[rt - 1], dim3((unsigned)(batch + p.items * p.slices * z)), dim3(kDownWaves * 64), list, 0, st);
+        return (int)(e != hipSuccess ? e : hipGetLastError());
+    });
+}
 int launch_adapter_down_digits(AdapterDown *d, const ActSource &act, int cq, void *digits, void *wide, bool plain, hipStream_t st)
 {
     const AdapterPlan &p = *d->plan;
     const pb_adapters &ad = *d->adapters;
     const int rt = rank_tiles(p.ranks), z = (p.ranks + rt - 1) / rt;
-    DownArgs u;
-    u.order = order_of(p, ad, d->index, act.batch, d->workspace);
-    u.M = ad.A; u.scale = nullptr; u.V = d->X;
-    u.out = reinterpret_cast<float *>(static_cast<char *>(d->workspace) + p.u_off);
-    u.length = d->layout->cols; u.rank = ad.rank; u.ranks = p.ranks; u.slices = p.slices;
+    DownArgs u, t;
+    down_args(p, ad, *d->layout, d->index, d->X, nullptr, act.batch, d->workspace, &u, &t);
     DigitsJob job;
     job.act = act;
     job.digits = static_cast<uint8_t *>(digits);

@@ -470,7 +470,7 @@ int pb_matmul_adapters(const void *packed, const float *scales, const pb_desc *d
     void *const ws = static_cast<char *>(workspace) + adapters_off(L, batch);
     int err = pb::launch_adapter_order(p, *adapters, index, batch, ws, st);
     if (err) return hip_status(err);
-    pb::AdapterDown down = {&p, adapters, &L, index, X, ws, false};
+    pb::AdapterDown down = {&p, adapters, &L, index, X, nullptr, ws, false};
     pb::Epilogue ep;
     ep.bias = bias;
     ep.pre = reinterpret_cast<float *>(static_cast<char *>(workspace) + pb::ws_gates_off(L, batch));
@@ -507,9 +507,10 @@ int pb_matmul_adapters_grad(const void *packed, const float *scales, const pb_de
     void *const ws = static_cast<char *>(workspace) + adapters_off(L, batch);
     int err = pb::launch_adapter_order(p, *adapters, index, batch, ws, st);
     // (u is needed for dB, t for dA and dX)
-    if (!err) err = pb::launch_adapter_down(p, *adapters, L, index, dB ? X : nullptr, dX || dA ? dY : nullptr, batch, ws, st);
+    pb::AdapterDown down = {&p, adapters, &L, index, dB ? X : nullptr, dX || dA ? dY : nullptr, ws, false};
     if (!err && dX)
-        err = pb::launch_grad(static_cast<const uint32_t *>(packed), scales, L, bits_used, dY, nullptr, batch, dX, workspace, st);
+        err = pb::launch_grad(static_cast<const uint32_t *>(packed), scales, L, bits_used, dY, nullptr, batch, dX, workspace, st, &down);
+    if (!err && !down.done) err = pb::launch_adapter_down(p, *adapters, L, index, down.X, down.dY, batch, ws, st);
     if (!err) err = pb::launch_adapter_grads(p, *adapters, L, index, X, dY, batch, dX, dA, dB, ws, st);
     return hip_status(err);
 }

@@ -23,87 +23,16 @@
 // 5.6 TB/s), digits 31 (157 MB, 5.0 TB/s).
 #include <type_traits>
 
-#include "pb_imma.h"
+#include "pb_grad.h"
 
 namespace pb {
 
 typedef int v2i __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef float float4_at4 __attribute__((ext_vector_type(4), aligned(4)));     // (global memory takes loads of 16 bytes at any multiple of four)
-
-constexpr int kNotFinite = INT32_MIN;      // in the place of an exponent: the vector's results are NaN
-
-// How a vector's gradients become integers: rint(dy 2^e4) with four digits, rint(dy 2^e3) with three
-struct Scaling { int e4, e3, wide, pad; };     // wide: four digits are needed
-
-// From the bits of the largest magnitude and the sum of squares of `count` values
-__device__ __forceinline__ Scaling scaling_of(uint32_t largest, double squares, int count)
-{
-    if (largest >= 0x7F800000u) return {kNotFinite, kNotFinite, 0, 0};
-    if (largest == 0) return {0, 0, 0, 0};
-    int e;
-    const double most = (double)__uint_as_float(largest);
-    const float f = frexpf(__uint_as_float(largest), &e);
-    // (three balanced digits hold 127 * 65536 + 127 * 256 + 127 = 8355711 < 2^23)
-    return {30 - e, 23 - e - (f * 8388608.0f > 8355000.0f ? 1 : 0), most * most * count > 144.0 * fmax(1.0, count / 4096.0) * squares ? 1 : 0, 0};
-}
-
-// The largest magnitude of a vector and the sum of its squares
-struct Size {
-    uint32_t most = 0;       // bits
-    double squares = 0.0;
-    __device__ void take(float v)
-    {
-        most = max(most, __float_as_uint(v) & 0x7FFFFFFFu);
-        squares = fma((double)v, (double)v, squares);
-    }
-    // thread `first` of `threads`: its share of y[0 .. rows)
-    __device__ void take(const float *y, int rows, int first, int threads)
-    {
-        const int fours = rows / 4;
-#pragma unroll 4
-        for (int i = first; i < fours; i += threads) {
-            const float4_at4 v = *reinterpret_cast<const float4_at4 *>(y + 4 * i);
-            take(v.x); take(v.y); take(v.z); take(v.w);
-        }
-        if (first < rows - 4 * fours) take(y[4 * fours + first]);
-    }
-    __device__ void over_wave()
-    {
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) {
-            most = max(most, (uint32_t)__shfl_xor((int)most, d));
-            squares += __shfl_xor(squares, d);
-        }
-    }
-    template <int WAVES>
-    __device__ void over_workgroup()       // (in thread 0)
-    {
-        __shared__ uint32_t s_max[WAVES];
-        __shared__ double s_sum[WAVES];
-        over_wave();
-        if ((threadIdx.x & 63) == 0) {
-            s_max[threadIdx.x >> 6] = most;
-            s_sum[threadIdx.x >> 6] = squares;
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-#pragma unroll
-            for (int w = 1; w < WAVES; ++w) {
-                most = max(most, s_max[w]);
-                squares += s_sum[w];
-            }
-        }
-    }
-};
 
 __global__ __launch_bounds__(1024) void k_grad_scalings(const float *__restrict__ dY, int rows, Scaling *__restrict__ scalings)
 {
-    const float *y = dY + (size_t)blockIdx.x * rows;
-    Size size;
-    size.take(y, rows, threadIdx.x, 1024);
-    size.over_workgroup<16>();
-    if (threadIdx.x == 0) scalings[blockIdx.x] = scaling_of(size.most, size.squares, rows);
+    scale_vector<16>(dY, rows, blockIdx.x, scalings);
 }
 
 // Gradients of the pre-activations [g; u] of H = act(g) u, and the scalings of their vectors
@@ -692,7 +621,7 @@ static const void *const kGradFn[5][2][2] = {PB_GRAD(1, false), PB_GRAD(4, false
 constexpr int kGradLds[5] = {GradShape<1>::LDS, GradShape<4>::LDS, GradShape<8>::LDS, GradShape<1>::LDS + kFusedLds, GradShape<1>::LDS + kFusedLds};
 
 int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, int bits_used, const float *dY, const GatedSource *gated,
-                int batch, float *dX, void *workspace, hipStream_t st)
+                int batch, float *dX, void *workspace, hipStream_t st, AdapterDown *down)
 {
     const GradPlan p = grad_plan(L, batch);
     char *const ws = static_cast<char *>(workspace);
@@ -709,7 +638,12 @@ int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, in
                            scalings);
         dY = gated->dpre;
     } else if (!gated && !own && !p.held) {
-        hipLaunchKernelGGL(k_grad_scalings, dim3((unsigned)batch), dim3(1024), 0, st, dY, L.rows, scalings);
+        if (down) {
+            err = launch_adapter_down_scalings(down, dY, batch, scalings, st);
+            if (err) return err;
+        } else {
+            hipLaunchKernelGGL(k_grad_scalings, dim3((unsigned)batch), dim3(1024), 0, st, dY, L.rows, scalings);
+        }
     }
     err = (int)hipGetLastError();
     if (err) return err;

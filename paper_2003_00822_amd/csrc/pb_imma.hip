@@ -292,10 +292,10 @@ int launch_imma(const uint32_t *packed, const float *scales, const Layout &L, in
     int cus;
     const hipError_t no_device = compute_units(&cus);
     if (no_device != hipSuccess) return (int)no_device;
-    // The adapters' first products go along with the digits up to 16 MB of activations, which saves a launch.  us, together / one after the other: 4096
-    // columns, 48 vectors 25.1 / 27.4, 512 vectors 55.2 / 57.4; 768 columns, 2017 vectors 47.0 / 50.2; but 4096 columns, 2048 vectors (34 MB) 246.4 / 244.4.
+    // The adapters' first products go along with the digits, a launch less.  us, together / one after the other: 4096 columns, 48 vectors 25.4 / 27.4,
+    // 512 vectors 55.0 / 57.4, 2048 vectors 238 / 241; 768 columns, 2017 vectors 46.2 / 50.2.
     auto make_digits = [&](bool plain) {
-        if (ep.down && nd == 4 && (long long)batch * L.cols <= 1 << 22) return launch_adapter_down_digits(ep.down, a.act, L.cq, digits, wide, plain, st);
+        if (ep.down && nd == 4) return launch_adapter_down_digits(ep.down, a.act, L.cq, digits, wide, plain, st);
         return launch_digits(X0, cols0, X1, cols1, batch, L, frac_bits, act_bits, digits, wide, nullptr, plain, st);
     };
     // Large batches of the operators: the kernel of pb_batch.hip where its workgroups, one per compute unit, fill 65 % of their rounds over the chip.
