@@ -838,3 +838,31 @@ def test_threads_share_layers(pb):
         t.join()
     torch.cuda.synchronize()
     assert not wrong, wrong
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [20, 90])
+def test_adapters_backward_one_gradient_at_a_time(pb, n):
+    c = AdapterCase(pb, 190, 350, 8, 8, n, "bits", 3, 20, "bf16", "mixed")
+    lin, d, desc = c.layer.lin, c.layer.lin.desc, c.adapters.desc()
+    X, dY, index = c.X.cuda(), c.dY.cuda(), c.index.cuda()
+    ws = torch.empty(pb.pb_adapters_workspace_bytes(d, desc, n), dtype=torch.uint8, device="cuda")
+    want = lin.adapted_grad(X, dY, c.adapters, index)
+    shapes = ((n, 350), (3, 20, 350), (3, 190, 20))
+    for asked in ((True, False, False), (False, True, False), (False, False, True), (False, True, True), (True, False, True), (True, True, False)):
+        outs = [torch.full(s, 7.0, device="cuda") if a else None for s, a in zip(shapes, asked)]
+        pb.pb_matmul_adapters_grad(lin.packed, lin.scales, d, 8, X, dY, n, desc, index, *outs, ws)
+        torch.cuda.synchronize()
+        for which, (got, w) in enumerate(zip(outs, want)):
+            if got is None:
+                continue
+            # (the waves may share the vectors of an adapter in another way: sums of up to n products in another order, their values bounded by
+            # sums of the terms' sizes, which are at most n times the largest ones')
+            if which == 0:
+                assert torch.equal(got, w)
+            else:
+                k = 1 if which == 1 else 2
+                u = (X.double() if k == 1 else dY.double()).abs().max() * n * 2.0 ** -24 * (n + 16)
+                factor = (c.dY.abs().double().sum(1).max() * c.B.abs().max().double() * c.scale.max().double()) if k == 1 else \
+                    (c.X.abs().double().sum(1).max() * c.A.abs().max().double() * c.scale.max().double())
+                assert (got.double() - w.double()).abs().max() <= u * factor
