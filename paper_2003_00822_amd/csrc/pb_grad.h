@@ -72,6 +72,39 @@ struct Size {
     }
 };
 
+// The parts of a split sum [split][total], in the order of the rows: values i and i + 1
+struct GradParts {
+    const float *parts;
+    float *dX;
+    size_t total;
+    int splits;
+};
+__device__ __forceinline__ void join_parts(const GradParts &p, size_t i)
+{
+    const float *const parts = p.parts;
+    float *const dX = p.dX;
+    const size_t total = p.total;
+    const int splits = p.splits;
+    if (i >= total) return;
+    if (total % 2 == 0) {
+        float2 v = *reinterpret_cast<const float2 *>(parts + i);
+#pragma unroll 8
+        for (int s = 1; s < splits; ++s) {
+            const float2 w = *reinterpret_cast<const float2 *>(parts + (size_t)s * total + i);
+            v.x += w.x;
+            v.y += w.y;
+        }
+        *reinterpret_cast<float2 *>(dX + i) = v;
+    } else {
+        for (size_t k = i; k < i + 2 && k < total; ++k) {
+            float v = parts[k];
+#pragma unroll 8
+            for (int s = 1; s < splits; ++s) v += parts[(size_t)s * total + k];
+            dX[k] = v;
+        }
+    }
+}
+
 // The scaling of vector n, by a workgroup of WAVES waves
 template <int WAVES>
 __device__ __forceinline__ void scale_vector(const float *__restrict__ dY, int rows, int n, Scaling *__restrict__ scalings)

@@ -545,29 +545,7 @@ __global__ __launch_bounds__(512) void k_grad(const GradArgs a)
     }
 }
 
-// The parts of a split sum, in the order of the rows
-__global__ __launch_bounds__(256) void k_grad_join(const float *__restrict__ parts, int splits, size_t total, float *__restrict__ dX)
-{
-    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 2;
-    if (i >= total) return;
-    if (total % 2 == 0) {
-        float2 v = *reinterpret_cast<const float2 *>(parts + i);
-#pragma unroll 8
-        for (int s = 1; s < splits; ++s) {
-            const float2 w = *reinterpret_cast<const float2 *>(parts + (size_t)s * total + i);
-            v.x += w.x;
-            v.y += w.y;
-        }
-        *reinterpret_cast<float2 *>(dX + i) = v;
-    } else {
-        for (size_t k = i; k < i + 2 && k < total; ++k) {
-            float v = parts[k];
-#pragma unroll 8
-            for (int s = 1; s < splits; ++s) v += parts[(size_t)s * total + k];
-            dX[k] = v;
-        }
-    }
-}
+__global__ __launch_bounds__(256) void k_grad_join(const GradParts p) { join_parts(p, ((size_t)blockIdx.x * 256 + threadIdx.x) * 2); }
 
 // ---------------------------------------------------------------------------------------------------------------
 
@@ -683,7 +661,9 @@ int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, in
     if (e != hipSuccess) return (int)e;
     if (p.splits > 1) {
         const size_t total = (size_t)batch * L.cols;
-        hipLaunchKernelGGL(k_grad_join, dim3((unsigned)((total + 511) / 512)), dim3(256), 0, st, parts, p.splits, total, dX);
+        const GradParts joined = {parts, dX, total, p.splits};
+        if (down && !down->done) return launch_adapter_down_join(down, joined, batch, st);
+        hipLaunchKernelGGL(k_grad_join, dim3((unsigned)((total + 511) / 512)), dim3(256), 0, st, joined);
         e = hipGetLastError();
     }
     return (int)e;

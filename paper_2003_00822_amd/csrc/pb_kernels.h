@@ -83,7 +83,7 @@ int launch_lstm_pointwise(const float *gates, const float *bias, const float *c_
 // pb_gated.hip: H[n][r] = act(pre[n][r]) pre[n][units + r]
 int launch_gated(const float *pre, int units, int gate, int batch, float *H, hipStream_t st);
 
-// pb_grad.hip: (`down`: adapters whose u and t are wanted; where the scalings have a launch, it does both) dX = dY W through the packed matrix (tiled layouts).  With `gated`, dY are the gradients of the pre-activations [g; u] of
+// pb_grad.hip: (`down`: adapters whose u and t are wanted; where the scalings or the join of the sum's parts have a launch, it does both) dX = dY W through the packed matrix (tiled layouts).  With `gated`, dY are the gradients of the pre-activations [g; u] of
 // H = act(g) u, which the call works out from dH and leaves in `dpre`.
 struct GatedSource {
     const float *pre, *dH;
@@ -107,7 +107,7 @@ int launch_adapter_order(const AdapterPlan &p, const pb_adapters &ad, const int3
 // u = A_k x (and t = scale_k B_k^T dY, if dY is given) of the ordered vectors, in parts
 int launch_adapter_down(const AdapterPlan &p, const pb_adapters &ad, const Layout &L, const int32_t *index, const float *X, const float *dY, int batch,
                         void *workspace, hipStream_t st);
-// The same for x beside k_digits<4>, or for x and dY (where given) beside k_grad_scalings, in one launch, which then is `done`
+// The same for x beside k_digits<4>, or for x and dY (where given) beside k_grad_scalings or k_grad_join, in one launch, which then is `done`
 struct AdapterDown {
     const AdapterPlan *plan;
     const pb_adapters *adapters;
@@ -119,6 +119,8 @@ struct AdapterDown {
 };
 struct ActSource;
 struct Scaling;
+struct GradParts;
+int launch_adapter_down_join(AdapterDown *down, const GradParts &joined, int batch, hipStream_t st);
 int launch_adapter_down_scalings(AdapterDown *down, const float *dY, int batch, Scaling *scalings, hipStream_t st);
 int launch_adapter_down_digits(AdapterDown *down, const ActSource &act, int cq, void *digits, void *wide, bool plain, hipStream_t st);
 // Y += scale_k B_k u; what launch_mfma needs to do it for one vector
