@@ -104,7 +104,8 @@ int pb_desc_init_layout(pb_desc *d, int rows, int cols, int bits, uint32_t layou
 
 /* Bytes the caller must allocate for `packed` (all B bitlayers, padded),
  * and for `workspace` of a call with `batch` activation vectors (bit planes,
- * plane statistics, and for pb_lstm_cell the gate pre-activations).
+ * plane statistics, and for pb_lstm_cell the gate pre-activations); a
+ * workspace serves every smaller batch too.
  * Return 0 if the descriptor is invalid. */
 size_t pb_packed_bytes(const pb_desc *d);
 size_t pb_workspace_bytes(const pb_desc *d, int batch);
@@ -275,7 +276,7 @@ int pb_gated_linear(const void *packed, const float *scales, const pb_desc *d, i
  * and rounded to fp32; where the sum over the rows is shared out, and for more than eight bitlayers, a few such sums are added in fp32, in the same
  * order every time.  A vector with a value that is not finite gets NaN everywhere.
  *   dY  [batch][rows] fp32, read only;  dX  [batch][cols] fp32, written; they do not overlap
- *   workspace: pb_grad_workspace_bytes(d, batch) bytes, overwritten (0 for what the call does not take)
+ *   workspace: pb_grad_workspace_bytes(d, batch) bytes, overwritten (0 for what the call does not take); they serve every smaller batch too
  * Tiled layouts only (PB_EINVAL for PB_LAYOUT_ROWMAJOR_V1). */
 size_t pb_grad_workspace_bytes(const pb_desc *d, int batch);
 int pb_matmul_grad(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *dY, int batch,
@@ -306,7 +307,8 @@ typedef struct pb_adapters {
  * The adapters' products take x as it is (not its fixed-point value) and run in fp32, whatever the adapters' type.
  *   index  [batch] int32, in any order; a vector whose index is outside [0, count) has no adapter.  NULL: adapter 0 for all
  *   bias   [rows] or NULL;  Y  [batch][rows] fp32, written, not overlapping an input
- *   workspace: pb_adapters_workspace_bytes(d, adapters, batch) bytes, overwritten (0 for a shape that is refused) */
+ *   workspace: pb_adapters_workspace_bytes(d, adapters, batch) bytes, overwritten (0 for a shape that is refused); they serve every smaller batch
+ *   of the same shape, with or without an index */
 size_t pb_adapters_workspace_bytes(const pb_desc *d, const pb_adapters *adapters, int batch);
 int pb_matmul_adapters(const void *packed, const float *scales, const pb_desc *d, int bits_used, const float *X, int batch,
                        const pb_adapters *adapters, const int32_t *index, const float *bias, float *Y, void *workspace, void *stream);

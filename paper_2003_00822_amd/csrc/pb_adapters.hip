@@ -679,26 +679,49 @@ __global__ __launch_bounds__(outer_waves(SPLIT) * 64) void k_adapter_grads(const
 
 // ---------------------------------------------------------------------------------------------------------------
 
+static int items_of(const pb_adapters &ad, int batch, bool indexed)
+{
+    return indexed ? (ad.count + batch / 16 < batch ? ad.count + batch / 16 : batch) : (batch + 15) / 16;
+}
+// Parts of the sums: about two workgroups per compute unit (one does not get more than its share of the memory's rate by much), each wave with
+// 64 summands or more.  A larger batch has no more parts than a smaller one.
+static int slices_of(const Layout &L, const pb_adapters &ad, int batch, bool indexed)
+{
+    const int most = L.rows > L.cols ? L.rows : L.cols, z = ((ad.rank + 15) / 16 + 3) / 4, items = items_of(ad, batch, indexed);
+    int slices = 1;
+    while (slices < (batch > kMany ? kPartsOfMany : 16) && items * z * slices < 384 && slices * 64 * kDownWaves < most) slices *= 2;
+    return slices;
+}
+static size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+static size_t down_bytes(const pb_adapters &ad, int batch, int slices) { return up256((size_t)batch * ((ad.rank + 15) / 16) * 64 * down_parts(slices)); }
+
 AdapterPlan adapter_plan(const Layout &L, const pb_adapters &ad, int batch, bool indexed)
 {
     AdapterPlan p;
-    const int tiles = (batch + 15) / 16;
-    p.items = indexed ? (ad.count + batch / 16 < batch ? ad.count + batch / 16 : batch) : tiles;
+    p.items = items_of(ad, batch, indexed);
     p.ranks = (ad.rank + 15) / 16;
-    // parts of the sums: about two workgroups per compute unit (one does not get more than its share of the memory's rate by much), each wave with
-    // 64 summands or more
-    const int most = L.rows > L.cols ? L.rows : L.cols, z = (p.ranks + 3) / 4;
-    p.slices = 1;
-    while (p.slices < (batch > kMany ? kPartsOfMany : 16) && p.items * z * p.slices < 384 && p.slices * 64 * kDownWaves < most) p.slices *= 2;
-    auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
-    const size_t down = up((size_t)batch * p.ranks * 64 * down_parts(p.slices));
-    p.items_off = up((size_t)batch * 4);
-    p.counts_off = up(p.items_off + (size_t)p.items * sizeof(Item));
+    p.slices = slices_of(L, ad, batch, indexed);
+    p.items_off = up256((size_t)batch * 4);
+    p.counts_off = up256(p.items_off + (size_t)p.items * sizeof(Item));
     p.starts_off = p.counts_off + 256;
-    p.u_off = up(p.starts_off + (size_t)(ad.count + 1) * 4);
-    p.t_off = p.u_off + down;
-    p.bytes = p.t_off + down;
+    p.u_off = up256(p.starts_off + (size_t)(ad.count + 1) * 4);
+    p.t_off = p.u_off + down_bytes(ad, batch, p.slices);
     return p;
+}
+// Room for this batch and every smaller one, whose sums may have more parts: the last batch of each number of parts needs most
+size_t adapter_bytes(const Layout &L, const pb_adapters &ad, int batch, bool indexed)
+{
+    size_t most = down_bytes(ad, batch, slices_of(L, ad, batch, indexed));
+    for (int parts = 16; parts > 4; parts /= 2) {
+        int with = 0, without = batch + 1;      // (batches that have as many parts, and those that do not)
+        while (without - with > 1) {
+            const int b = (with + without) / 2;
+            (slices_of(L, ad, b, indexed) >= parts ? with : without) = b;
+        }
+        const size_t bytes = with ? down_bytes(ad, with, parts) : 0;
+        most = bytes > most ? bytes : most;
+    }
+    return adapter_plan(L, ad, batch, indexed).u_off + 2 * most;
 }
 
 static Order order_of(const AdapterPlan &p, const pb_adapters &ad, const int32_t *index, int batch, void *workspace)

@@ -448,7 +448,7 @@ size_t pb_adapters_workspace_bytes(const pb_desc *d, const pb_adapters *ad, int 
     pb::Layout L;
     if (check_desc(d, &L) != PB_OK || batch < 1 || batch > PB_MAX_BATCH) return 0;
     if (!ad || ad->count < 1 || ad->count > PB_MAX_ADAPTERS || ad->rank < 1 || ad->rank > PB_MAX_RANK) return 0;
-    const size_t with = pb::adapter_plan(L, *ad, batch, true).bytes, without = pb::adapter_plan(L, *ad, batch, false).bytes;
+    const size_t with = pb::adapter_bytes(L, *ad, batch, true), without = pb::adapter_bytes(L, *ad, batch, false);
     return adapters_off(L, batch) + (with > without ? with : without);
 }
 

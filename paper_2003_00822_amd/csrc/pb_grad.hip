@@ -552,13 +552,25 @@ __global__ __launch_bounds__(256) void k_grad_join(const GradParts p) { join_par
 // How a call is shared out; the workspace holds [scalings][digits][parts of the split sum]
 struct GradPlan {
     int wm, blocks, ks, steps, splits, steps_per_split, held;       // held: 0, or the digits are made by k_grad
-    size_t digits_off, parts_off, bytes;
+    size_t digits_off, parts_off;
 };
 constexpr int kGradCus = 256;
+// A workspace has to serve every smaller batch too, and the fastest number of parts goes up and down with the batch: the parts together get no more room
+// than this, which grows with the batch.  64 MB, or three times dX (more parts than that paid in 3 of 1000 drawn calls, by 3 % of the estimated time).
+static int least_parts(int steps) { return (steps + 1023) / 1024; }       // (int32 sums: 65536 rows)
+static size_t parts_room(const Layout &L, int steps, int batch)
+{
+    const size_t one = (size_t)batch * L.cols * 4, most = (size_t)((steps + 1) / 2), least = (size_t)least_parts(steps);
+    const size_t few = (least > 3 ? least : 3) * one, room = few > (64u << 20) ? few : 64u << 20;
+    return most > 1 ? (most * one < room ? most * one : room) : 0;
+}
+static size_t digits_offset(int batch) { return ((size_t)batch * sizeof(Scaling) + 255) & ~(size_t)255; }
+static size_t digits_bytes(int steps, int batch) { return (size_t)((batch + 15) / 16) * (size_t)steps * 4096; }
 static GradPlan grad_plan(const Layout &L, int batch)
 {
     GradPlan p;
     p.steps = (L.rt_count + 3) / 4;
+    const size_t room = parts_room(L, p.steps, batch);
     double least_time = 1e30;
     // The shape: one wave along the vectors for up to 32, four for up to 64, eight for more, or one all the same where that is estimated to be faster
     // (the digits then need no launch).  us, digits in launches of their own / in k_grad: 670 x 2642, 71 vectors 20.0 / 13.8; 1024 x 1024, 128 vectors
@@ -570,9 +582,10 @@ static GradPlan grad_plan(const Layout &L, int batch)
         // Parts of the sum: rounds of workgroups over the chip (one per compute unit), each of so many us for its start and end and for a step; more
         // than one part costs the way of the parts through memory and a launch, digits that do not fit a workgroup a launch or two.
         const double step = wm == 8 ? 0.67 : (wm == 4 ? 0.75 : 1.5);
-        for (int splits = (p.steps + 1023) / 1024, n = 0; n < 64; ++splits, ++n) {       // (int32 sums: 65536 rows)
+        for (int splits = least_parts(p.steps), n = 0; n < 64; ++splits, ++n) {
             const int each = ((p.steps + splits - 1) / splits + ks - 1) / ks * ks, parts = (p.steps + each - 1) / each;   // (whole buffers)
             if (parts < splits && n) continue;
+            if (parts > 1 && (size_t)parts * batch * L.cols * 4 > room) break;
             const bool fits = held && each * held <= kFusedSteps * 4;
             const double rounds = (double)(((long long)blocks * rows_of * parts + kGradCus - 1) / kGradCus);
             const double time = (fits ? 0.0 : 4.0 + (batch > 16 ? 2.0 : 0.0)) + rounds * (3.0 + (fits ? 2.0 : 0.0) + step * each) +
@@ -583,13 +596,16 @@ static GradPlan grad_plan(const Layout &L, int batch)
             }
         }
     }
-    auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
-    p.digits_off = up((size_t)batch * sizeof(Scaling));
-    p.parts_off = p.digits_off + (p.held ? 0 : (size_t)((batch + 15) / 16) * (size_t)p.steps * 4096);
-    p.bytes = p.parts_off + (p.splits > 1 ? up((size_t)p.splits * batch * L.cols * 4) : 0);
+    p.digits_off = digits_offset(batch);
+    p.parts_off = p.digits_off + (p.held ? 0 : digits_bytes(p.steps, batch));
     return p;
 }
-size_t grad_workspace_bytes(const Layout &L, int batch) { return grad_plan(L, batch).bytes; }
+// (the digits count also where k_grad makes them: a smaller batch may have them in memory)
+size_t grad_workspace_bytes(const Layout &L, int batch)
+{
+    const int steps = (L.rt_count + 3) / 4;
+    return digits_offset(batch) + digits_bytes(steps, batch) + ((parts_room(L, steps, batch) + 255) & ~(size_t)255);
+}
 
 #define PB_GRAD(WM, FUSED) {{reinterpret_cast<const void *>(k_grad<1, false, WM, FUSED>), reinterpret_cast<const void *>(k_grad<1, true, WM, FUSED>)}, \
                             {reinterpret_cast<const void *>(k_grad<2, false, WM, FUSED>), reinterpret_cast<const void *>(k_grad<2, true, WM, FUSED>)}}

@@ -90,7 +90,7 @@ struct GatedSource {
     float *dpre;
     int gate;
 };
-size_t grad_workspace_bytes(const Layout &L, int batch);
+size_t grad_workspace_bytes(const Layout &L, int batch);      // (not less than those of a smaller batch)
 int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, int bits_used, const float *dY, const GatedSource *gated,
                 int batch, float *dX, void *workspace, hipStream_t st, AdapterDown *down = nullptr);
 
@@ -99,9 +99,10 @@ struct AdapterPlan {
     int items;             // tiles of up to sixteen vectors of one adapter, at most
     int ranks;             // rank tiles of sixteen
     int slices;            // parts of the sums of u and t
-    size_t items_off, counts_off, starts_off, u_off, t_off, bytes;
+    size_t items_off, counts_off, starts_off, u_off, t_off;
 };
 AdapterPlan adapter_plan(const Layout &L, const pb_adapters &ad, int batch, bool indexed);
+size_t adapter_bytes(const Layout &L, const pb_adapters &ad, int batch, bool indexed);     // (not less than those of a smaller batch)
 // The order of the vectors (by adapter) and its tiles; nothing to do without an index or for few vectors
 int launch_adapter_order(const AdapterPlan &p, const pb_adapters &ad, const int32_t *index, int batch, void *workspace, hipStream_t st);
 // u = A_k x (and t = scale_k B_k^T dY, if dY is given) of the ordered vectors, in parts
