@@ -104,7 +104,8 @@ int pb_desc_init_layout(pb_desc *d, int rows, int cols, int bits, uint32_t layou
 
 /* Bytes the caller must allocate for `packed` (all B bitlayers, padded),
  * and for `workspace` of a call with `batch` activation vectors (bit planes,
- * plane statistics, and for pb_lstm_cell the gate pre-activations); a
+ * plane statistics, and for pb_lstm_cell and pb_gated_linear the gate
+ * pre-activations and sums); a
  * workspace serves every smaller batch too.
  * Return 0 if the descriptor is invalid. */
 size_t pb_packed_bytes(const pb_desc *d);

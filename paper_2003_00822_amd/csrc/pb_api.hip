@@ -75,6 +75,14 @@ private:
     pthread_mutex_t *m;
 };
 
+// What a gated block's large batches need behind the workspace of pb_matmul: the second word of its sums in fp64 (the first one is in the place of the
+// pre-activations)
+size_t gated_bytes(const pb::Layout &L, int batch)
+{
+    if (L.layout != PB_LAYOUT_TILE16_GATES_V1 || batch <= pb::kBatchFrom) return 0;
+    return ((size_t)batch * (size_t)L.rows * 4 + 255) & ~(size_t)255;
+}
+
 int hip_status(int err)
 {
     if (err == 0) return PB_OK;
@@ -117,7 +125,7 @@ size_t pb_workspace_bytes(const pb_desc *d, int batch)
 {
     pb::Layout L;
     if (check_desc(d, &L) != PB_OK || batch < 1 || batch > PB_MAX_BATCH) return 0;
-    return pb::workspace_bytes(L, batch);
+    return pb::workspace_bytes(L, batch) + gated_bytes(L, batch);
 }
 
 int pb_quantize_pack_mode(const float *W, const pb_desc *d, int quantizer, void *packed, float *scales, void *stream)
@@ -373,6 +381,7 @@ int pb_gated_linear(const void *packed, const float *scales, const pb_desc *d, i
         ep.gate = gate;
         ep.h_out = H;
         ep.pre = reinterpret_cast<float *>(static_cast<char *>(workspace) + pb::ws_gates_off(L, batch));
+        ep.more = reinterpret_cast<float *>(static_cast<char *>(workspace) + pb::workspace_bytes(L, batch));
         return matmul_common(packed, scales, d, bits_used, X, d->cols, nullptr, 0, batch, pre, nullptr, workspace, stream, ep);
     }
     const Issuing issuing(workspace);

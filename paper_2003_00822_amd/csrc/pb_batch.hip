@@ -33,7 +33,7 @@ struct BatchGrid {
 };
 
 template <int Q, bool IL, int EPI>
-__global__ __launch_bounds__(512) void k_batch(const I8Args a, const BatchGrid grid, float *const partial)
+__global__ __launch_bounds__(512) void k_batch(const I8Args a, const BatchGrid grid, float *const low, float *const high)
 {
     extern __shared__ __align__(16) unsigned char s_codes[];
     __shared__ int s_ones[kBatchTiles][kTileRows];
@@ -211,12 +211,18 @@ __global__ __launch_bounds__(512) void k_batch(const I8Args a, const BatchGrid g
                     const bool live = row_ok && n < a.act.batch;
                     int d[4] = {acc[0][nt][c], acc[1][nt][c], acc[2][nt][c], 0};
                     if constexpr (ND == 4) d[3] = acc[ND - 1][nt][c];
-                    float y = (float)(scaled_sum<4>(g, d, sum1, ND == 4) * a.out_scale);
-                    float *const sum = partial + (size_t)n * a.R + row;
-                    if (live && f > 0) y += *sum;             // (the thread's own: earlier groups of bitlayers)
-                    if (live && !g.last) *sum = y;
-                    if (g.last) {
-                        y += bias;
+                    double v = scaled_sum<4>(g, d, sum1, ND == 4);
+                    const size_t o = (size_t)n * a.R + row;
+                    // (the thread's own: the sum of the earlier groups of bitlayers, an fp64 value in two words)
+                    if (live && f > 0) v += __hiloint2double((int)__float_as_uint(high[o]), (int)__float_as_uint(low[o]));
+                    if (!g.last) {
+                        if (live) {
+                            high[o] = __uint_as_float((uint32_t)__double2hiint(v));
+                            low[o] = __uint_as_float((uint32_t)__double2loint(v));
+                        }
+                    } else {
+                        float y = (float)(v * a.out_scale);
+                        if (a.bias) y += bias;
                         if constexpr (EPI == kGated)
                             s_out[(wave * kGroupVectors + (at >> 4) * 4 + c) * kBatchRow + (jj & 3) * 33 + nt * 4 + (jj >> 2)] = y;
                         else if (live) a.Y[(size_t)n * a.R + row] = y;
@@ -266,7 +272,7 @@ int batch_workgroups(int rt_count, int batch)
     return ((rt_count + kBatchTiles - 1) / kBatchTiles) * ((batch + kBatchVectors - 1) / kBatchVectors);
 }
 
-int launch_imma_batch(const I8Args &a, bool il, float *partial, hipStream_t st)
+int launch_imma_batch(const I8Args &a, bool il, float *low, float *high, hipStream_t st)
 {
     const int gated = a.gate >= 0, q = a.m > 4;
     const void *fn = kBatchFn[gated][q][il];
@@ -280,7 +286,7 @@ int launch_imma_batch(const I8Args &a, bool il, float *partial, hipStream_t st)
     grid.blocks = (a.rt_count + kBatchTiles - 1) / kBatchTiles;
     grid.rows_of = (a.act.batch + kBatchVectors - 1) / kBatchVectors;
     grid.workgroups = grid.blocks * grid.rows_of;
-    void *args[] = {const_cast<I8Args *>(&a), &grid, &partial};
+    void *args[] = {const_cast<I8Args *>(&a), &grid, &low, &high};
     const hipError_t e = hipLaunchKernel(fn, dim3((unsigned)grid.workgroups), dim3(512), args, (size_t)kBatchLds, st);
     return (int)(e != hipSuccess ? e : hipGetLastError());
 }

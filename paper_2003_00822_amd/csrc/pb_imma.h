@@ -432,9 +432,9 @@ int launch_imma_tile(int shape, const I8Args &a, int nd, bool il, hipStream_t st
 // Whether it takes a gated block's act(g) u along (the other shapes' registers are full)
 inline bool gated_tile(int shape) { return shape == 0; }
 
-// The kernel for large batches of the gated block and the adapters (pb_batch.hip): its workgroups, its launch (`partial`: [batch][R], used where
-// there are several groups of bitlayers)
+// The kernel for large batches of the gated block and the adapters (pb_batch.hip): its workgroups, its launch.  `low`, `high`: [batch][R] each, the two
+// words of the sums of several groups of bitlayers in fp64; a.Y may be one of them
 int batch_workgroups(int rt_count, int batch);
-int launch_imma_batch(const I8Args &a, bool il, float *partial, hipStream_t st);
+int launch_imma_batch(const I8Args &a, bool il, float *low, float *high, hipStream_t st);
 
 }  // namespace pb

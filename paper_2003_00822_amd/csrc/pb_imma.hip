@@ -302,10 +302,10 @@ int launch_imma(const uint32_t *packed, const float *scales, const Layout &L, in
     // us with it / with the kernels below, 8 bitlayers, digits included: 8192 x 2048, 300 vectors (192 workgroups) 31.0 / 34.7; 24600 x 4096, 65
     // (193) 46.1 / 52.7; 16384 x 4096, 140 (256) 49.2 / 53.0; 2048 x 8192, 2048 (256) 111 / 138; 6000 x 600, 2000 (752) 60 / 95; but 2048 x 8192, 1000 (128)
     // 80 / 72, 4096 x 4096, 512 (128) 50 / 42, 12000 x 8192, 5 bitlayers, 100 (94) 71 / 51.
-    const int large = ep.pre && nd == 4 && batch > 64 ? batch_workgroups(L.rt_count, batch) : 0;
+    const int large = ep.pre && nd == 4 && batch > kBatchFrom ? batch_workgroups(L.rt_count, batch) : 0;
     if (large * 20 >= (large + cus - 1) / cus * cus * 13 && large) {
         const int e = make_digits(true);
-        return e ? e : launch_imma_batch(a, il, ep.pre, st);
+        return e ? e : launch_imma_batch(a, il, ep.pre, a.Y ? a.Y : ep.more, st);
     }
     int way = pick_way(c, prepared, cus);
     if (way == kFusedNt && (A || ep.fused())) way = kFused1;

@@ -37,6 +37,7 @@ struct AdapterRows {
     int rank, count, type, nparts;
 };
 struct AdapterDown;
+constexpr int kBatchFrom = 64;           // the kernel for large batches takes more vectors than this
 constexpr int kAdapterRowsRank = 16;     // (32 cost scratch memory in two of the kernels)
 struct Epilogue {
     const float *bias = nullptr;   // [rows] or null
@@ -45,6 +46,7 @@ struct Epilogue {
     float *h_out = nullptr, *c_out = nullptr;
     int gate = -1;                 // 0 or more: fused gated block (a pb_gate)
     float *pre = nullptr;          // non-null: room for [batch][rows], and the kernel for large batches of pb_batch.hip may be taken
+    float *more = nullptr;         // as much room again, where there is no Y and that kernel may be taken (more than kBatchFrom vectors)
     AdapterDown *down = nullptr;   // adapters whose u = A_k x is wanted: where the activations' digits have a launch, it does both
     const AdapterRows *adapter = nullptr;   // (one vector, tiled layouts but the pairs')
     bool fused() const { return c_prev || gate >= 0; }
