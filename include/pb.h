@@ -258,7 +258,7 @@ int pb_lstm_cell(const void *packed, const float *scales, const pb_desc *d, int 
 /* A gated block: the two projections of its input packed as one matrix, rows = 2F, row r < F the gate and row F + r the
  * value of unit r.  With [g ; u] = W x + bias (the product of pb_matmul),
  *   H[n][r] = act(g[r]) * u[r],
- * act a pb_gate, in fp32.  PB_GATE_GELU is the tanh form, 0.5 v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))).
+ * act a pb_gate, in fp32; NaN (from a bias) stays NaN.  PB_GATE_GELU is the tanh form, 0.5 v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))).
  *   X     [batch][cols] fp32, bias [2F] or NULL: read only
  *   H     [batch][F], written
  *   pre   [batch][2F] or NULL: the pre-activations [g ; u], written (what the backward pass needs)

@@ -72,10 +72,11 @@ __device__ __forceinline__ void lstm_quad(float y, int lane, float c_old, float 
 
 // Gate of a gated block, H = act(g) u, and its slope.  GELU in its tanh form: 0.5 v (1 + tanh(t / 2)) = v / (1 + exp(-t)), t = sqrt(8 / pi) (v + 0.044715 v^3),
 // so that all but ReLU are one logistic function, which as a quotient keeps its relative precision far from 0 (0.5 tanh + 0.5 does not).
+// NaN stays NaN, in the slope too: the comparisons are those that it fails.
 constexpr float kGelu1 = 1.5957691216057308f, kGelu3 = kGelu1 * 0.044715f;
 __device__ __forceinline__ float gate_act(int gate, float v)
 {
-    if (gate == PB_GATE_RELU) return fmaxf(v, 0.0f);
+    if (gate == PB_GATE_RELU) return v <= 0.0f ? 0.0f : v;
     const float t = gate == PB_GATE_GELU ? v * fmaf(kGelu3, v * v, kGelu1) : v;
     const float s = 1.0f / (1.0f + expf(-t));
     return gate == PB_GATE_SIGMOID ? s : v * s;
@@ -89,13 +90,13 @@ __device__ __forceinline__ float gated_quad(int gate, float y)
 __device__ __forceinline__ void gate_with_slope(int gate, float v, float *a, float *da)
 {
     if (gate == PB_GATE_RELU) {
-        *a = fmaxf(v, 0.0f);
-        *da = v > 0.0f ? 1.0f : 0.0f;
+        *a = v <= 0.0f ? 0.0f : v;
+        *da = v > 0.0f ? 1.0f : *a;
         return;
     }
     const float t = gate == PB_GATE_GELU ? v * fmaf(kGelu3, v * v, kGelu1) : v;
     const float ex = expf(-t), s = 1.0f / (1.0f + ex);
-    const float ds = s > 0.0f ? s * (ex * s) : 0.0f;      // s (1 - s), without the difference
+    const float ds = s == 0.0f ? 0.0f : s * (ex * s);      // s (1 - s), without the difference
     if (gate == PB_GATE_SIGMOID) {
         *a = s;
         *da = ds;
