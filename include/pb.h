@@ -272,8 +272,9 @@ int pb_gated_linear(const void *packed, const float *scales, const pb_desc *d, i
 /* Gradient of pb_matmul with respect to its activations, the packed matrix being frozen:
  *   dX[n][c] = sum_r dY[n][r] w[r][c],   w = sum_{i < bits_used} scales[i] * bit_i,
  * with the same bits_used as in the forward call; the conversion to fixed point counts as the identity (frac_bits and act_bits do
- * not matter).  dY enters as integers: off by at most 2^-30 of its vector's largest magnitude, or 2^-23 of it in groups of sixteen vectors of
- * batches above 32 where no value is above 12 sqrt(max(1, rows / 4096)) times the root of its vector's mean square.  The sums of products are exact
+ * not matter).  dY enters as integers: off by at most 2^-30 of its vector's largest magnitude, or 2^-23 / 0.995 of it in groups of sixteen vectors
+ * of batches above 32 where no value is above L times the root of its vector's mean square; L = sqrt(rows) / 4 below 2304 rows, else
+ * 12 sqrt(max(1, rows / 4096)) (rows = 2F values in pb_gated_linear_grad).  The sums of products are exact
  * and rounded to fp32; where the sum over the rows is shared out, and for more than eight bitlayers, a few such sums are added in fp32, in the same
  * order every time.  A vector with a value that is not finite gets NaN everywhere.
  *   dY  [batch][rows] fp32, read only;  dX  [batch][cols] fp32, written; they do not overlap

@@ -20,7 +20,8 @@ __device__ __forceinline__ Scaling scaling_of(uint32_t largest, double squares, 
     const double most = (double)__uint_as_float(largest);
     const float f = frexpf(__uint_as_float(largest), &e);
     // (three balanced digits hold 127 * 65536 + 127 * 256 + 127 = 8355711 < 2^23)
-    return {30 - e, 23 - e - (f * 8388608.0f > 8355000.0f ? 1 : 0), most * most * count > 144.0 * fmax(1.0, count / 4096.0) * squares ? 1 : 0, 0};
+    const double limit = count < 2304 ? count / 16.0 : 144.0 * fmax(1.0, count / 4096.0);
+    return {30 - e, 23 - e - (f * 8388608.0f > 8355000.0f ? 1 : 0), most * most * count > limit * squares ? 1 : 0, 0};
 }
 
 // The largest magnitude of a vector and the sum of its squares

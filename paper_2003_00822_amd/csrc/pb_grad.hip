@@ -5,10 +5,11 @@
 // split into four balanced byte digits, g = sum_d 256^d s_d with s_d in [-128, 127]: the bytes of (g + 0x808080) ^ 0x808080, because
 // 0x808080 = sum_(d < 3) 256^d 128.  The rounding (half a unit, at most 2^-30 of the vector's largest gradient) is the only one before the last
 // step: |s code| <= 2^14, so a sum over 65536 rows is exact in int32, and the digits' sums are put together in fp64.
-// Batches, which the matrix instructions bound, take three digits (half a unit: at most 2^-23 of the largest gradient) where no vector of
-// sixteen has a value above 12 sqrt(max(1, R / 4096)) times the root of its mean square: a result over R rows is then off by
-// 12 * 2^-22 / sqrt(12) = 8e-7 sqrt(max(1, R / 4096)) of the results' root mean square at most, typically a quarter of it.  (A product in fp32 is
-// off by 1.75e-8 sqrt(R), measured from 1500 to 21844 rows: 1.1e-6 at 4096.)
+// Batches, which the matrix instructions bound, take three digits (half a unit: at most 2^-23 / 0.995 of the largest gradient; 0.995: a largest value
+// that three balanced digits just do not hold is halved) where no vector of sixteen has a value above L times the root of its mean square,
+//   L = sqrt(R) / 4 for a sum over R < 2304 rows, 12 up to 4096, 12 sqrt(R / 4096) for more:
+// a result is then off by L 2^-22 / sqrt(12) = 6.9e-8 L of the results' root mean square at most, typically a quarter of it, which is no more than a product
+// in fp32 is off by: 1.75e-8 sqrt(R), measured from 1500 to 21844 rows.
 //
 // Few vectors (and small matrices): k_grad makes the digits itself, from the rows of its part of the sum; each part has a scale of its own, and the parts
 // are added in fp32 anyway.  Else k_grad_digits leaves them in memory, for all of the columns' workgroups.

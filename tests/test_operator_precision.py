@@ -51,3 +51,70 @@ def test_several_groups_of_bitlayers_give_the_product_of_matmul(pb, rows, cols, 
             none = torch.full((batch,), -1, dtype=torch.int32, device="cuda")
             adapters = pb.Adapters(torch.zeros((1, 1, cols), device="cuda"), torch.zeros((1, rows, 1), device="cuda"))
             assert torch.equal(lin.adapted(X, adapters, none, m, bias=b), want)
+
+
+def spread(seed, batch, rows):
+    """Gradients: in groups of sixteen vectors, in turn, normal values, products of three normal values, one large value beside small ones in one vector of
+    the group, and all of these."""
+    g = torch.Generator().manual_seed(seed)
+    dY = torch.randn((batch, rows), generator=g)
+    heavy = dY * torch.randn((batch, rows), generator=g) * torch.randn((batch, rows), generator=g)
+    single = torch.randn((batch, rows), generator=g) * 1e-6
+    single[torch.arange(batch), torch.randint(0, rows, (batch,), generator=g)] = 1.0
+    n = torch.arange(batch)
+    kind = (n // 16) % 4
+    dY = torch.where(((kind == 1) | (kind == 3) & (n % 3 == 0))[:, None], heavy, dY)
+    dY = torch.where((((kind == 2) & (n % 16 == 5)) | (kind == 3) & (n % 3 == 1))[:, None], single, dY)
+    return (dY * 10.0 ** torch.randint(-6, 7, (batch, 1), generator=g)).cuda()
+
+
+def digits_are_enough(dX, dY, of_column, weight):
+    """dX[n, c] = weight dY[n, of_column[c]] to within half a unit of dY's integers and the rounding of the result."""
+    d64 = dY.double()
+    batch, rows = dY.shape
+    largest = d64.abs().amax(dim=1)
+    ratio = largest ** 2 * rows / (d64 ** 2).sum(dim=1)
+    limit = rows / 16 if rows < 2304 else 144 * max(1.0, rows / 4096)
+    assert ((ratio / limit - 1).abs() > 1e-9).all()            # (else the side that a vector is on hangs on the rounding of the sums)
+    wide = torch.repeat_interleave(torch.stack([(group > limit).any() for group in ratio.split(16)]), 16)[:batch]
+    assert wide.any() and not wide.all()
+    half = torch.where(wide, torch.tensor(2.0 ** -30, dtype=torch.float64, device="cuda"),
+                       torch.tensor(2.0 ** -23 / 0.995, dtype=torch.float64, device="cuda")) * largest
+    want = d64[:, of_column] * weight
+    assert ((dX.double() - want).abs() <= half[:, None] * weight + 2.0 ** -24 * want.abs()).all()
+
+
+# rows = columns (one weight in each), bits, batch, layout: digits and scalings in a launch of their own, in one, in the kernel of the product
+DIGITS = [(600, 8, 2000, BITS), (600, 3, 1999, PAIRS), (1100, 8, 1100, BITS), (2300, 8, 300, BITS), (2300, 4, 330, PAIRS), (2560, 4, 520, BITS), (4500, 8, 90, BITS),
+          (4096, 8, 60, BITS), (4096, 3, 50, PAIRS), (300, 8, 100, BITS)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,bits,batch,layout", DIGITS)
+def test_gradients_have_the_digits_that_their_values_need(pb, rows, bits, batch, layout):
+    """One weight per row and column: every value of dY comes out by itself."""
+    perm = torch.randperm(rows, generator=torch.Generator().manual_seed(4)).cuda()
+    W = torch.zeros((rows, rows), device="cuda")
+    W[perm, torch.arange(rows, device="cuda")] = 1.0
+    lin = pb.PackedLinear(W, bits, layout=layout)
+    weight = float(lin.scales[bits - 1]) * int(lin.unpack().max())
+    dY = spread(5, batch, rows)
+    digits_are_enough(lin.grad(dY), dY, perm, weight)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("units,bits,batch,layout", [(300, 8, 2000, GATES), (551, 8, 1000, BITS), (1200, 4, 300, GATES), (2048, 8, 60, PAIRS)])
+def test_gradients_of_gated_blocks_have_the_digits_that_their_values_need(pb, units, bits, batch, layout):
+    rows = 2 * units
+    perm = torch.randperm(rows, generator=torch.Generator().manual_seed(4)).cuda()
+    W = torch.zeros((rows, rows), device="cuda")
+    W[perm, torch.arange(rows, device="cuda")] = 1.0
+    lin = pb.PackedLinear(W, bits, layout=layout)
+    weight = float(lin.scales[bits - 1]) * int(lin.unpack().max())
+    # in every other group of sixteen vectors the values are all of the same size (ReLU passes them on)
+    pre, dH = rand(6, batch, rows), spread(7, batch, units)
+    even = torch.arange(batch, device="cuda") // 16 % 2 == 0
+    pre[even] = 1.0
+    dH[even] = 1.0 + 0.1 * rand(8, int(even.sum()), units).clamp(-3, 3)
+    dX, dpre = lin.gated_grad(pre, dH, pb.PB_GATE_RELU)
+    digits_are_enough(dX, dpre, perm, weight)
