@@ -398,7 +398,7 @@ size_t pb_grad_workspace_bytes(const pb_desc *d, int batch)
     return pb::grad_workspace_bytes(L, batch);
 }
 
-// Checks that the gradient calls share; the caller's lock is held
+// Checks that the gradient calls share
 static int check_grad(const void *packed, const float *scales, const pb_desc *d, int bits_used, int batch, const void *workspace, pb::Layout *L)
 {
     const int rc = check_desc(d, L);

@@ -261,9 +261,10 @@ __global__ __launch_bounds__(512) void k_batch(const I8Args a, const BatchGrid g
 
 // ---------------------------------------------------------------------------------------------------------------
 
-#define PB_BATCH(E) {{reinterpret_cast<const void *>(k_batch<1, false, E>), reinterpret_cast<const void *>(k_batch<1, true, E>)}, \
-                     {reinterpret_cast<const void *>(k_batch<2, false, E>), reinterpret_cast<const void *>(k_batch<2, true, E>)}}
-static const void *const kBatchFn[2][2][2] = {PB_BATCH(kStore), PB_BATCH(kGated)};
+// (a gated block on the pairs layout leaves its pre-activations in memory for k_gated)
+static const void *const kBatchFn[2][2] = {{reinterpret_cast<const void *>(k_batch<1, false, kStore>), reinterpret_cast<const void *>(k_batch<1, true, kStore>)},
+                                           {reinterpret_cast<const void *>(k_batch<2, false, kStore>), reinterpret_cast<const void *>(k_batch<2, true, kStore>)}};
+static const void *const kBatchGatedFn[2] = {reinterpret_cast<const void *>(k_batch<1, false, kGated>), reinterpret_cast<const void *>(k_batch<2, false, kGated>)};
 constexpr int kBatchLds = 2 * kBatchBuffer;
 static_assert(kBatchVectors * kBatchRow * 4 <= kBatchLds, "the results of a gated block in the place of the codes");
 
@@ -275,7 +276,7 @@ int batch_workgroups(int rt_count, int batch)
 int launch_imma_batch(const I8Args &a, bool il, float *low, float *high, hipStream_t st)
 {
     const int gated = a.gate >= 0, q = a.m > 4;
-    const void *fn = kBatchFn[gated][q][il];
+    const void *fn = gated ? kBatchGatedFn[q] : kBatchFn[q][il];
     static bool declared[2][2][2];      // (more than the default 64 KB of LDS)
     if (!__atomic_load_n(&declared[gated][q][il], __ATOMIC_RELAXED)) {
         const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kBatchLds);
