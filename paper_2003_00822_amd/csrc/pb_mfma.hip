@@ -581,10 +581,11 @@ struct Variant {
 #define PB_VARIANT(NQ, MAXS, RU) \
     {NQ, MAXS, RU, reinterpret_cast<const void *>(k_mfma<NQ, MAXS, RU>), reinterpret_cast<const void *>(k_mfma<NQ, MAXS, RU, kGatedBlock>), \
      reinterpret_cast<const void *>(k_mfma<NQ, MAXS, RU, kAdapted>)}
+#define PB_VARIANT_PLAIN(NQ, MAXS, RU) {NQ, MAXS, RU, reinterpret_cast<const void *>(k_mfma<NQ, MAXS, RU>), nullptr, nullptr}
 static const Variant kVariants[] = {
     PB_VARIANT(1, 16, 1), PB_VARIANT(1, 16, 2), PB_VARIANT(1, 16, 4),
     PB_VARIANT(2, 16, 1), PB_VARIANT(2, 16, 2), PB_VARIANT(2, 16, 3),
-    PB_VARIANT(4, 8, 1),  PB_VARIANT(4, 8, 2),
+    PB_VARIANT_PLAIN(4, 8, 1), PB_VARIANT_PLAIN(4, 8, 2),      // (for the sweeps over the variants only)
     PB_VARIANT(4, 16, 1),
 };
 constexpr int kNumVariants = sizeof(kVariants) / sizeof(kVariants[0]);
@@ -658,7 +659,7 @@ static int resident_workgroups(int variant, int S)
             const Variant &o = kVariants[i];
             if (o.nq != kVariants[variant].nq || o.maxs != kVariants[variant].maxs) continue;
             for (const void *fn : {o.fn, o.gated, o.adapted})
-                if (hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)stage_bytes(S)) != hipSuccess) return 0;
+                if (fn && hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)stage_bytes(S)) != hipSuccess) return 0;
         }
     }
     if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kVariants[variant].fn, S * 64, stage_bytes(S)) != hipSuccess)
@@ -707,8 +708,9 @@ int launch_mfma(const uint32_t *packed, const float *scales, const Layout &L, in
     void *args[] = {&h.packed, &h.X0, &h.packed_bytes, &h.flags, &h.cols0, &h.layer_step, &h.round_step,
                     &h.rounds_per_wg, &h.rt_count, &h.cq, &h.m, &a};
     a.adapter = ep.adapter ? *ep.adapter : AdapterRows{};
-    const hipError_t e = hipLaunchKernel(ep.gate >= 0 ? run.gated : (ep.adapter ? run.adapted : run.fn), dim3((unsigned)wgs), dim3((unsigned)S * 64), args,
-                                         planes ? 0 : stage_bytes(S), st);
+    const void *const fn = ep.gate >= 0 ? run.gated : (ep.adapter ? run.adapted : run.fn);
+    if (!fn) return (int)hipErrorInvalidValue;
+    const hipError_t e = hipLaunchKernel(fn, dim3((unsigned)wgs), dim3((unsigned)S * 64), args, planes ? 0 : stage_bytes(S), st);
     return (int)(e != hipSuccess ? e : hipGetLastError());
 }
 
