@@ -443,7 +443,10 @@ __device__ __forceinline__ void adapter_up(const UpArgs &a, int column, int item
         for (int rt0 = 0; rt0 < a.ranks; rt0 += RT) {
             float sum[RT];
 #pragma unroll
-            for (int t = 0; t < RT; ++t) sum[t] = down_at<decltype(parts)::value>(a.parts, a.ranks, vector, min(rt0 + t, a.ranks - 1), i) * s;
+            for (int t = 0; t < RT; ++t) {
+                sum[t] = down_at<decltype(parts)::value>(a.parts, a.ranks, vector, min(rt0 + t, a.ranks - 1), i) * s;
+                if ((rt0 + t) * 16 + i >= a.rank) sum[t] = 0.0f;      // (whatever the scale is)
+            }
 #pragma unroll
             for (int t = 0; t < RT; ++t)
                 if (rt0 + t < a.ranks) s_u[((rt0 + t) * 16 + i) * kUpRow + v] = sum[t];

@@ -118,3 +118,39 @@ def test_gradients_of_gated_blocks_have_the_digits_that_their_values_need(pb, un
     dH[even] = 1.0 + 0.1 * rand(8, int(even.sum()), units).clamp(-3, 3)
     dX, dpre = lin.gated_grad(pre, dH, pb.PB_GATE_RELU)
     digits_are_enough(dX, dpre, perm, weight)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch", [1, 5, 40])
+@pytest.mark.parametrize("rank", [5, 16, 21])
+def test_a_scale_that_is_infinite_gives_infinities_and_stays_by_itself(pb, batch, rank):
+    """scale B (A x) with an infinite scale: of the sign of B A x, whatever the rank is padded to."""
+    lin = pb.PackedLinear(rand(1, 70, 90) * 0.1, 8, max_batch=batch)
+    A, B, X = rand(2, 2, rank, 90).abs(), rand(3, 2, 70, 1).expand(2, 70, rank).contiguous(), rand(4, batch, 90).abs()
+    index = torch.arange(batch, device="cuda", dtype=torch.int32) % 2
+    Y = lin.adapted(X, pb.Adapters(A, B, torch.tensor([float("inf"), 1.0], device="cuda")), index)
+    sign = B[0, :, 0].sign()                                    # (all ranks of a row have its sign, u is positive)
+    assert torch.equal(Y[::2], (sign * float("inf")).expand(Y[::2].shape))
+    clean = lin.adapted(X, pb.Adapters(A, B, torch.ones(2, device="cuda")), index)
+    assert torch.equal(Y[1::2], clean[1::2])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act_bits", [8, 16])
+@pytest.mark.parametrize("batch", [1, 7, 100])
+@pytest.mark.parametrize("layout", [BITS, PAIRS, GATES])
+def test_adapters_beside_narrow_activations(pb, batch, act_bits, layout):
+    lin = pb.PackedLinear(rand(1, 200, 700) * 0.05, 8, max_batch=batch, layout=layout, act_bits=act_bits, frac_bits=5 if act_bits == 8 else 12)
+    X, A, B = rand(2, batch, 700), rand(3, 3, 11, 700) * 0.1, rand(4, 3, 200, 11) * 0.1
+    index = torch.arange(batch, device="cuda", dtype=torch.int32) % 4          # (3: none)
+    Y = lin.adapted(X, pb.Adapters(A, B), index)
+    plain = torch.empty_like(Y)
+    pb.pb_matmul(lin.packed, lin.scales, lin.desc, 8, X, batch, plain, lin.workspace)
+    want, terms = plain.double(), plain.double().abs()
+    for n in range(batch):
+        if n % 4 < 3:
+            want[n] += B[n % 4].double() @ (A[n % 4].double() @ X[n].double())
+            # a sum of K fp32 products is K U of its terms off at most; one rounding of the sum
+            terms[n] += (700 + 11 + 8) * (B[n % 4].abs().double() @ (A[n % 4].abs().double() @ X[n].abs().double())) + 2 * want[n].abs()
+    assert ((Y.double() - want).abs() <= 2.0 ** -24 * terms).all()
+    assert torch.equal(Y[3::4], plain[3::4])
