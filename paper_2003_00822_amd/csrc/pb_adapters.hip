@@ -8,9 +8,9 @@
 // row i (column i) of the two operands at position kb of the sum, and gets rows 4 kb .. 4 kb + 3 of column i of the result.  Which
 // summand stands at which position is free as long as both operands agree, so lanes load neighbouring summands with wide loads.
 // Bound: memory and latencies (the products of 2048 vectors of rank 16 with 4096 columns take 2 us of the chip's fp32 matrix rate).  us (rocprofv3):
-// 8192 x 4096, six adapters of rank 32 in fp16, 2048 vectors: down 18.2 (34 MB of vectors, 1.9 TB/s), up 32.1 (134 MB, 4.2 TB/s), order 8.0;
-// 8698 x 6860, 36 of rank 42 in fp16, 25 vectors: down 16.1 (u and t), up 8.8, outer 22.6 (94 MB of gradients written, 4.2 TB/s); 1024 x 1024, rank 8, one
-// vector: down 3.9, up 3.7, which is little more than a launch each.
+// 8192 x 4096, six adapters of rank 32 in fp16, 2048 vectors: u beside the activations' digits 22.5 (77 MB fetched, 37 written), up 28.5 (71 fetched and 60
+// written of the 134 MB of Y, 4.7 TB/s), order 7.0; 4096 x 4096, 4 of rank 16 in bf16, 2048 vectors: u and t beside the scalings 21.0 (100 MB), gradients 27.7
+// (101 and 32 MB); 1024 x 1024, rank 8, one vector: down 3.7, which is little more than a launch (its up is behind the product).
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include <stdint.h>

@@ -5,9 +5,9 @@
 // LDS: two buffers of 64 KB (a chunk of 512 columns each).  While a wave multiplies one buffer it turns the words of its row tile for the other
 // one into codes, step by step between the products.  Per chunk and wave: 8 KB of words and 24 KB of digits (three of four, see pb_imma.h) from
 // memory, 64 KB of codes from LDS, 192 matrix instructions.
-// Bound: the matrix instructions (16 cycles each); LDS and the vector-memory pipeline are busy for about three quarters of that.
-// us: 8192 x 4096, 8 bitlayers, 2048 vectors 196 (2.10 POP/s in three digits); a gated block of 21844 x 4096, 1024 vectors 286 (1.92 POP/s; its 1368
-// workgroups are 5.3 rounds over the chip).
+// Bound: the matrix instructions and what does not run beside them.  us (rocprofv3): 8192 x 4096, 8 bitlayers, 2048 vectors 190 (2.17 POP/s in three digits),
+// the matrix pipelines busy for 57 % of the compute units' cycles, waves waiting for 35 % of theirs, at 2.0 GHz; a gated block of 21844 x 4096,
+// 1024 vectors 288 (1.91 POP/s; its 1368 workgroups are 5.3 rounds over the chip), 53 % and 35 %.  The first calls on an idle card take up to a fifth longer.
 #include <type_traits>
 
 #include "pb_imma.h"

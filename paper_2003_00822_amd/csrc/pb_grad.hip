@@ -19,9 +19,10 @@
 // way out: its 16 lanes read eight rows of sixteen bytes, and lane i receives byte i of each.
 //
 // Bound: the packed words for few vectors, the matrix instructions for batches.  us (rocprofv3): 8192 x 8192, 8 bitlayers, 4 vectors: k_grad 17.0 (3.9 TB/s
-// of words) and k_grad_join 3.9; 6 bitlayers, 768 vectors: k_grad 138 (2.25 POP/s in three digits; a library product of 8-bit integers of that
-// size reaches 1.83), scalings 7.5, digits 8.3, join 14.4; 21844 x 4096, 8 bitlayers, 1024 vectors: k_grad 261 (2.1 POP/s), k_gated_grad 40 (224 MB,
-// 5.6 TB/s), digits 31 (157 MB, 5.0 TB/s).
+// of words: 67.5 MB fetched) and k_grad_join 3.9; 6 bitlayers, 768 vectors: k_grad 136 (2.28 POP/s in three digits; a library product of 8-bit integers
+// 8192^3 reaches 1.83), the matrix pipelines busy for 60 % of the compute units' cycles, waves waiting for 36 % of theirs, at 2.07 GHz, scalings 7.3, digits 8.2,
+// join 14.4; 21844 x 4096, 8 bitlayers, 1024 vectors: k_grad 253 (2.17 POP/s; 66 % and 39 %), in the first calls on an idle card up to 309, k_gated_grad 39
+// (136 MB fetched and 91 written, 5.8 TB/s), digits 31 (137 and 68 MB, 6.6 TB/s).
 #include <type_traits>
 
 #include "pb_grad.h"

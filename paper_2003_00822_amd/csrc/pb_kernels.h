@@ -23,12 +23,6 @@ int launch_prep(const float *X0, int cols0, const float *X1, int cols1, int batc
 int launch_matvec(const uint32_t *packed, const float *scales, const Layout &L, int bits_used, int frac_bits,
                   const uint32_t *planes, const int *meta, int batch, float *Y, long long *A, hipStream_t st);
 
-// pb_mfma.hip: the whole of Algorithm 2 in one launch on the matrix cores, for ONE activation vector (the tiled layouts but
-// the pairs layout).  Activations come from X0 / X1 (converted and bit-transposed inside the kernel) or, if `planes` is
-// non-null, from bit planes that launch_prep left in memory.  Exactly one of Y / A is non-null.
-// What follows the product in the same launch: bias and ReLU before the store of Y, or (PB_LAYOUT_TILE16_GATES_V1
-// only) the LSTM cell update, which writes h_out / c_out [batch][H] instead of Y, or a gated block's act(g) u, which writes
-// h_out [batch][rows / 2] and, where wanted, the pre-activations to Y.
 // What a single vector's adapter adds to it in k_mfma: scale_k B_k u, u being there in parts (pb_adapters.hip)
 struct AdapterRows {
     const void *B;
@@ -36,9 +30,16 @@ struct AdapterRows {
     const int32_t *index;
     int rank, count, type, nparts;
 };
-struct AdapterDown;
-constexpr int kBatchFrom = 64;           // the kernel for large batches takes more vectors than this
 constexpr int kAdapterRowsRank = 16;     // (32 cost scratch memory in two of the kernels)
+struct AdapterDown;
+
+// pb_mfma.hip: the whole of Algorithm 2 in one launch on the matrix cores, for ONE activation vector (the tiled layouts but
+// the pairs layout).  Activations come from X0 / X1 (converted and bit-transposed inside the kernel) or, if `planes` is
+// non-null, from bit planes that launch_prep left in memory.  Exactly one of Y / A is non-null.
+// What follows the product in the same launch: bias and ReLU before the store of Y, or (PB_LAYOUT_TILE16_GATES_V1
+// only) the LSTM cell update, which writes h_out / c_out [batch][H] instead of Y, or a gated block's act(g) u, which writes
+// h_out [batch][rows / 2] and, where wanted, the pre-activations to Y.
+constexpr int kBatchFrom = 64;           // the kernel for large batches takes more vectors than this
 struct Epilogue {
     const float *bias = nullptr;   // [rows] or null
     int relu = 0;
@@ -85,8 +86,9 @@ int launch_lstm_pointwise(const float *gates, const float *bias, const float *c_
 // pb_gated.hip: H[n][r] = act(pre[n][r]) pre[n][units + r]
 int launch_gated(const float *pre, int units, int gate, int batch, float *H, hipStream_t st);
 
-// pb_grad.hip: (`down`: adapters whose u and t are wanted; where the scalings or the join of the sum's parts have a launch, it does both) dX = dY W through the packed matrix (tiled layouts).  With `gated`, dY are the gradients of the pre-activations [g; u] of
-// H = act(g) u, which the call works out from dH and leaves in `dpre`.
+// pb_grad.hip: dX = dY W through the packed matrix (tiled layouts).  With `gated`, dY are the gradients of the pre-activations [g; u] of
+// H = act(g) u, which the call works out from dH and leaves in `dpre`.  `down`: adapters whose u and t are wanted; where the scalings or the join of
+// the sum's parts have a launch, it does both.
 struct GatedSource {
     const float *pre, *dH;
     float *dpre;

@@ -407,12 +407,13 @@ class PackedLinear:
         pb_matmul_acc_pairs(self.packed, self.desc, m, X, batch, A, torch.empty_like(self.workspace))
         return A
 
-    # The calls below have workspaces of their own: they take any stream and thread, and a captured graph keeps its own.
+    # The calls below have workspaces of their own: they take any stream and thread, and a captured graph keeps its own.  Like __call__ they know nothing of
+    # autograd: what they return has no history, also where an input requires a gradient; gated_grad, grad and adapted_grad are the backward passes.
 
     def gated(self, X: torch.Tensor, gate: int = PB_GATE_SILU, bits_used: int | None = None, bias: torch.Tensor | None = None,
               keep: bool = False):
         """H = act(g) u with [g; u] = W x + bias: the block's two projections packed as one matrix, gate rows first.  With `keep` also the
-        pre-activations [g; u], for gated_grad."""
+        pre-activations [g; u], for gated_grad.  The results have no autograd history."""
         return _methods["gated"](self, X, gate, bits_used, bias, keep)
 
     def gated_grad(self, pre: torch.Tensor, dH: torch.Tensor, gate: int = PB_GATE_SILU, bits_used: int | None = None):
@@ -425,7 +426,8 @@ class PackedLinear:
 
     def adapted(self, X: torch.Tensor, adapters: Adapters, index: torch.Tensor | None, bits_used: int | None = None,
                 bias: torch.Tensor | None = None):
-        """W x + bias + scale_k B_k A_k x with k = index[n] (int32; outside [0, count): no adapter; None: adapter 0 for all)."""
+        """W x + bias + scale_k B_k A_k x with k = index[n] (int32; outside [0, count): no adapter; None: adapter 0 for all).  The result has no autograd
+        history: the gradients of x, A and B are adapted_grad."""
         return _methods["adapted"](self, X, adapters, index, bits_used, bias)
 
     def adapted_grad(self, X: torch.Tensor, dY: torch.Tensor, adapters: Adapters, index: torch.Tensor | None, bits_used: int | None = None,
