@@ -280,12 +280,9 @@ int launch_imma_batch(const I8Args &a, bool il, float *low, float *high, hipStre
 {
     const int gated = a.gate >= 0, q = a.m > 4;
     const void *fn = gated ? kBatchGatedFn[q] : kBatchFn[q][il];
-    static bool declared[2][2][2];      // (more than the default 64 KB of LDS)
-    if (!__atomic_load_n(&declared[gated][q][il], __ATOMIC_RELAXED)) {
-        const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kBatchLds);
-        if (e != hipSuccess) return (int)e;
-        __atomic_store_n(&declared[gated][q][il], true, __ATOMIC_RELAXED);
-    }
+    static uint64_t declared[2][2][2];
+    const int d = declare_lds(fn, kBatchLds, &declared[gated][q][il]);
+    if (d) return d;
     BatchGrid grid;
     grid.blocks = (a.rt_count + kBatchTiles - 1) / kBatchTiles;
     grid.rows_of = (a.act.batch + kBatchVectors - 1) / kBatchVectors;

@@ -666,15 +666,11 @@ int launch_grad(const uint32_t *packed, const float *scales, const Layout &L, in
     if (gated) a.gated = *gated;
     const int shape = gated_inside ? 4 : p.held ? 3 : (p.wm == 8 ? 2 : p.wm / 4), wide = bits_used > 4, il = is_pairs(L.layout);
     const void *fn = kGradFn[shape][wide][il];
-    static bool declared[5][2][2];      // (more than the default 64 KB of LDS)
-    hipError_t e = hipSuccess;
-    if (!__atomic_load_n(&declared[shape][wide][il], __ATOMIC_RELAXED)) {
-        e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kGradLds[shape]);
-        if (e != hipSuccess) return (int)e;
-        __atomic_store_n(&declared[shape][wide][il], true, __ATOMIC_RELAXED);
-    }
+    static uint64_t declared[5][2][2];
+    err = declare_lds(fn, (size_t)kGradLds[shape], &declared[shape][wide][il]);
+    if (err) return err;
     void *args[] = {&a};
-    e = hipLaunchKernel(fn, dim3((unsigned)a.workgroups), dim3(512), args, (size_t)kGradLds[shape], st);
+    hipError_t e = hipLaunchKernel(fn, dim3((unsigned)a.workgroups), dim3(512), args, (size_t)kGradLds[shape], st);
     if (e == hipSuccess) e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
     if (p.splits > 1) {

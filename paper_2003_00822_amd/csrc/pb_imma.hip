@@ -153,7 +153,6 @@ static int per_unit(const void *fn, int threads, size_t lds, size_t stage, int *
 {
     int v = __atomic_load_n(slot, __ATOMIC_RELAXED);
     if (v > 0) return v;
-    if (stage && hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kMaxStage) != hipSuccess) return 0;
     if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&v, fn, threads, stage) != hipSuccess) return 0;
     auto at_most = [&](int n) { v = n < 1 ? 1 : (n < v ? n : v); };
     if (v > 1 && threads > 256) {
@@ -335,6 +334,11 @@ int launch_imma(const uint32_t *packed, const float *scales, const Layout &L, in
     const int S = (L.cq + a.chunks_per_wave - 1) / a.chunks_per_wave;
     const size_t lds = is_fused(way) ? stage_bytes(c, tm) : 0;
     static int cache[4][3][2][2][kStreams][17][24];   // (the last index: LDS in steps of 6 KB)
+    if (lds > 32 * 1024) {
+        static uint64_t declared[4][3][2][2][kStreams];
+        const int d = declare_lds(fn, kMaxStage, &declared[epi][ndi][q][il][way]);
+        if (d) return d;
+    }
     int most = per_unit(fn, S * 64, (size_t)stream_lds(nd, tm, epi), lds, &cache[epi][ndi][q][il][way][S][lds / 6144]);
     if (most < 1) return (int)hipErrorInvalidValue;
     if (is_fused(way) && most > fused_per_cu(S)) most = fused_per_cu(S);

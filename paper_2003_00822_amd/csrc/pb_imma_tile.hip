@@ -73,14 +73,10 @@ int launch_imma_tile(int shape, const I8Args &a, int nd, bool il, hipStream_t st
     const int epi = a.A ? kSums : (a.c_prev ? kCell : kStore), q = (epi != kSums && a.m > 4) ? 1 : 0, ndi = nd == 4 ? 2 : nd - 1;
     const bool gated = gated_tile(shape) && a.gate >= 0;
     const void *fn = gated ? kGatedTileFn[ndi][q] : kTileFn[shape][ndi][epi][q][il];
-    static bool declared_of[2][kTileShapes][3][3][2][2];
-    auto &declared = declared_of[gated];
+    static uint64_t declared[2][kTileShapes][3][3][2][2];
     if (!fn) return (int)hipErrorInvalidValue;
-    if (!__atomic_load_n(&declared[shape][ndi][epi][q][il], __ATOMIC_RELAXED)) {
-        const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kTileLds);
-        if (e != hipSuccess) return (int)e;
-        __atomic_store_n(&declared[shape][ndi][epi][q][il], true, __ATOMIC_RELAXED);
-    }
+    const int d = declare_lds(fn, kTileLds, &declared[gated][shape][ndi][epi][q][il]);
+    if (d) return d;
     const TileShape &t = kTile[shape];
     int rows_per_wg = tile_rows(t, a.m, epi == kSums);
     const int vpt = 16 / nd, tiles = (a.act.batch + vpt - 1) / vpt;

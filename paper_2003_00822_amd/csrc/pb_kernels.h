@@ -8,6 +8,20 @@
 
 namespace pb {
 
+// More dynamic LDS than the default 64 KB is declared once per kernel and GPU, `bytes` being the most that its launches use.  `devices`: the kernel's own, a
+// bit for each GPU on which it has been (beyond 64 of them: at every call).
+inline int declare_lds(const void *fn, size_t bytes, uint64_t *devices)
+{
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return (int)e;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (__atomic_load_n(devices, __ATOMIC_RELAXED) & bit) return 0;
+    e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == hipSuccess) __atomic_fetch_or(devices, bit, __ATOMIC_RELAXED);
+    return (int)e;
+}
+
 // pb_quantize.hip
 int launch_quantize_pack(const float *W, const Layout &L, int quantizer, uint32_t *packed, float *scales,
                          hipStream_t st);

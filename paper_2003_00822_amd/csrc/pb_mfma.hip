@@ -641,6 +641,15 @@ static int pick_ring(int vi, int units)
 // Dynamic LDS of a workgroup of S waves: the staging area of the activation transpose.
 static size_t stage_bytes(int S) { return (size_t)S * kStageRows * sizeof(uint2); }
 
+// (a workgroup's dynamic LDS may exceed the default limit of 64 KB, a compute unit of this chip has 160 KB)
+static int declare_stage(int variant, int more, int S)
+{
+    static uint64_t declared[kNumVariants][3];
+    const Variant &v = kVariants[variant];
+    const void *const fn = more == kGatedBlock ? v.gated : (more == kAdapted ? v.adapted : v.fn);
+    return stage_bytes(S) > 32 * 1024 ? declare_lds(fn, stage_bytes(v.maxs), &declared[variant][more]) : 0;
+}
+
 // Workgroups of S waves that fit on the device at once (occupancy does not change while the process lives, so it
 // is looked up once per kernel variant and workgroup size).
 static int resident_workgroups(int variant, int S)
@@ -652,16 +661,7 @@ static int resident_workgroups(int variant, int S)
     int dev = 0, cus = 0, per_cu = 0;
     if (hipGetDevice(&dev) != hipSuccess) return 0;
     if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 0;
-    // (a workgroup's dynamic LDS may exceed the default limit of 64 KB, a compute unit of this chip has 160 KB:
-    // declared for this variant and its siblings of other ring depths, one of which is the one launched)
-    if (stage_bytes(S) > 32 * 1024) {
-        for (int i = 0; i < kNumVariants; ++i) {
-            const Variant &o = kVariants[i];
-            if (o.nq != kVariants[variant].nq || o.maxs != kVariants[variant].maxs) continue;
-            for (const void *fn : {o.fn, o.gated, o.adapted})
-                if (fn && hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)stage_bytes(S)) != hipSuccess) return 0;
-        }
-    }
+    if (declare_stage(variant, kPlain, S)) return 0;
     if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kVariants[variant].fn, S * 64, stage_bytes(S)) != hipSuccess)
         return 0;
     v = cus * per_cu;
@@ -704,12 +704,16 @@ int launch_mfma(const uint32_t *packed, const float *scales, const Layout &L, in
     if (wgs > L.rt_count) wgs = L.rt_count;
     h.rounds_per_wg = (L.rt_count + wgs - 1) / wgs;
     wgs = (L.rt_count + h.rounds_per_wg - 1) / h.rounds_per_wg;
-    const Variant &run = kVariants[pick_ring(vi, h.rounds_per_wg * bits_used)];
+    const int ring = pick_ring(vi, h.rounds_per_wg * bits_used);
+    const Variant &run = kVariants[ring];
     void *args[] = {&h.packed, &h.X0, &h.packed_bytes, &h.flags, &h.cols0, &h.layer_step, &h.round_step,
                     &h.rounds_per_wg, &h.rt_count, &h.cq, &h.m, &a};
     a.adapter = ep.adapter ? *ep.adapter : AdapterRows{};
-    const void *const fn = ep.gate >= 0 ? run.gated : (ep.adapter ? run.adapted : run.fn);
+    const int more = ep.gate >= 0 ? kGatedBlock : (ep.adapter ? kAdapted : kPlain);
+    const void *const fn = more == kGatedBlock ? run.gated : (more == kAdapted ? run.adapted : run.fn);
     if (!fn) return (int)hipErrorInvalidValue;
+    const int d = planes ? 0 : declare_stage(ring, more, S);
+    if (d) return d;
     const hipError_t e = hipLaunchKernel(fn, dim3((unsigned)wgs), dim3((unsigned)S * 64), args, planes ? 0 : stage_bytes(S), st);
     return (int)(e != hipSuccess ? e : hipGetLastError());
 }
