@@ -105,8 +105,7 @@ int pb_desc_init_layout(pb_desc *d, int rows, int cols, int bits, uint32_t layou
 /* Bytes the caller must allocate for `packed` (all B bitlayers, padded),
  * and for `workspace` of a call with `batch` activation vectors (bit planes,
  * plane statistics, and for pb_lstm_cell and pb_gated_linear the gate
- * pre-activations and sums); a
- * workspace serves every smaller batch too.
+ * pre-activations and sums); a workspace serves every smaller batch too.
  * Return 0 if the descriptor is invalid. */
 size_t pb_packed_bytes(const pb_desc *d);
 size_t pb_workspace_bytes(const pb_desc *d, int batch);
@@ -274,9 +273,10 @@ int pb_gated_linear(const void *packed, const float *scales, const pb_desc *d, i
  * with the same bits_used as in the forward call; the conversion to fixed point counts as the identity (frac_bits and act_bits do
  * not matter).  dY enters as integers: off by at most 2^-30 of its vector's largest magnitude, or 2^-23 / 0.995 of it in groups of sixteen vectors
  * of batches above 32 where no value is above L times the root of its vector's mean square; L = sqrt(rows) / 4 below 2304 rows, else
- * 12 sqrt(max(1, rows / 4096)) (rows = 2F values in pb_gated_linear_grad).  The sums of products are exact
- * and rounded to fp32; where the sum over the rows is shared out, and for more than eight bitlayers, a few such sums are added in fp32, in the same
- * order every time.  A vector with a value that is not finite gets NaN everywhere.
+ * 12 sqrt(max(1, rows / 4096)) (rows = 2F values in pb_gated_linear_grad).  The sums of products are exact and rounded to fp32; where the
+ * sum over the rows is shared out, and where the bitlayers are taken in groups (eight, then six at a time; each by itself if the scales do not halve), a
+ * few such sums are added in fp32, in the same order every time: off by the roundings of the groups' terms, which for a small negative weight are
+ * larger than the weight.  A vector with a value that is not finite gets NaN everywhere.
  *   dY  [batch][rows] fp32, read only;  dX  [batch][cols] fp32, written; they do not overlap
  *   workspace: pb_grad_workspace_bytes(d, batch) bytes, overwritten (0 for what the call does not take); they serve every smaller batch too
  * Tiled layouts only (PB_EINVAL for PB_LAYOUT_ROWMAJOR_V1). */

@@ -122,18 +122,22 @@ def digits_of(dY, batch):
 
 
 def matrix(layer, m):
-    return torch.from_numpy(layer.matrix(m)).cuda()
+    """The matrix, and the sizes of its terms: eight bitlayers, then six at a time are summed exactly and rounded by themselves (a small negative code is a
+    difference of two such terms)."""
+    weights = [float(layer.scales[i]) * layer.layers[i].reshape(layer.rows, layer.cols).astype(np.float64) for i in range(m)]
+    groups = [sum(weights[:8])] + [sum(weights[i:i + 6]) for i in range(8, m, 6)]
+    return torch.from_numpy(layer.matrix(m)).cuda(), torch.from_numpy(sum(np.abs(g) for g in groups)).cuda()
 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("rows,cols,bits,m,batch,layout", GRADS)
 def test_gradients(pb, rows, cols, bits, m, batch, layout):           # noqa: F811
     layer = Layer(pb, rows, cols, bits, LAYOUTS[layout])
-    dY, W = spread(torch.Generator().manual_seed(21), batch, rows), matrix(layer, m)
+    dY, (W, terms) = spread(torch.Generator().manual_seed(21), batch, rows), matrix(layer, m)
     d64 = dY.double()
     # parts of the sum of two steps of 64 rows or more, and up to three groups of bitlayers: each rounded, and added one after the other
     parts = ((rows + 127) // 128) * (1 + (m > 8) + (m > 14))
-    tol = digits_of(d64, batch) * W.abs().sum(dim=0) + 2 * parts * U * (d64.abs() @ W.abs())
+    tol = digits_of(d64, batch) * terms.sum(dim=0) + 2 * parts * U * (d64.abs() @ terms)
     got = layer.lin.grad(dY, m)
     assert ((got.double() - d64 @ W).abs() <= tol).all()
     assert torch.equal(layer.lin.grad(dY, m), got)
@@ -181,7 +185,7 @@ def test_gated_blocks(pb, units, cols, bits, m, batch, act_bits):     # noqa: F8
 def test_gated_blocks_backward(pb, units, cols, bits, m, batch, act_bits):       # noqa: F811
     layer = Layer(pb, 2 * units, cols, bits, LAYOUTS["gates"])
     g = torch.Generator().manual_seed(23)
-    pre, dH, W = torch.randn((batch, 2 * units), generator=g).cuda() * 2, spread(g, batch, units), matrix(layer, m)
+    pre, dH, (W, terms) = torch.randn((batch, 2 * units), generator=g).cuda() * 2, spread(g, batch, units), matrix(layer, m)
     parts = ((2 * units + 127) // 128) * (1 + (m > 8) + (m > 14))
     for gate in (1, 2):
         dX, dpre = layer.lin.gated_grad(pre, dH, gate, m)
@@ -191,7 +195,7 @@ def test_gated_blocks_backward(pb, units, cols, bits, m, batch, act_bits):      
         size = 1 + v.abs() * (1 + v * v)
         close(dpre, torch.cat([d * u * da, d * a], dim=1).cpu().numpy(), (32 * U * torch.cat([(d * u).abs() * size, d.abs() * size], dim=1)).cpu().numpy(), "dpre")
         d64 = dpre.double()
-        tol = digits_of(d64, batch) * W.abs().sum(dim=0) + 2 * parts * U * (d64.abs() @ W.abs())
+        tol = digits_of(d64, batch) * terms.sum(dim=0) + 2 * parts * U * (d64.abs() @ terms)
         assert ((dX.double() - d64 @ W).abs() <= tol).all()
 
 
